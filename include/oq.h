@@ -63,8 +63,9 @@ typedef enum {
   OQ_ERR_ARG = -7        /* another invalid argument (enum value, step index, ...)  */
 } oq_status;
 
-/* Output element type of the dequantizing epilogue. */
-typedef enum { OQ_OUT_F16 = 0, OQ_OUT_BF16 = 1 } oq_out_dtype;
+/* Output element type of the dequantizing epilogue, and element type of the
+ * attention and cache operands (OQ_OUT_F32: outputs of oq_kv4_gather only). */
+typedef enum { OQ_OUT_F16 = 0, OQ_OUT_BF16 = 1, OQ_OUT_F32 = 2 } oq_out_dtype;
 
 /* Largest Hadamard block the rotation kernel accepts. */
 #define OQ_MAX_HAD_BLOCK 16384
@@ -386,6 +387,60 @@ int oq_w4a8_gemm_i32(const int8_t* Xq8, int64_t M, const uint8_t* Wq, int64_t N,
                      int32_t* acc, int64_t ldc, void* stream);
 
 /* ------------------------------------------------------------------------ */
+/* W8A8: 8 bits on both sides, for linears that 4-bit weights cost too much    */
+/* ------------------------------------------------------------------------ */
+/*
+ * oq_quantize_weights_i8 -- oq_quantize_weights at 8 bits (eq:scale, eq:quant
+ * with k = 8): Wq8 device int8 [N][K] in [-127, 127], 16-byte aligned, w_scale
+ * fp32 [N] = max / 127.  Identical to oq_rotate_quantize_act_i8 with s_t = 1 on
+ * the weight's rows; arguments, limits and errors as there.
+ */
+int oq_quantize_weights_i8(const void* W_u, int64_t N, int64_t K, int64_t ldw, int32_t had_block,
+                           int8_t* Wq8, float* w_scale, void* stream);
+
+/*
+ * oq_w8a8_linear / oq_w8a8_gemm_i32 -- the W4A8 calls with the weight in 8-bit
+ * codes [N][K] too: acc[i][n] = sum_k q8[i][k] * wq8[n][k] exactly in int32
+ * (any int8 codes: |acc| <= 2^14 K <= 2^28), Y[i][n] = round_to_out(float(acc) *
+ * x_scale[i] * w_scale[n] + bias[n]).  Shapes, alignment and errors as the W4A4
+ * calls.
+ */
+int oq_w8a8_linear(const int8_t* Xq8, const float* x_scale, int64_t M,
+                   const int8_t* Wq8, const float* w_scale, const void* bias,
+                   int64_t N, int64_t K, void* Y, int64_t ldy, int32_t out_dtype,
+                   void* stream);
+int oq_w8a8_gemm_i32(const int8_t* Xq8, int64_t M, const int8_t* Wq8, int64_t N, int64_t K,
+                     int32_t* acc, int64_t ldc, void* stream);
+
+/* ------------------------------------------------------------------------ */
+/* Attention over packed prompts                                             */
+/* ------------------------------------------------------------------------ */
+/*
+ * oq_attention_prompt -- softmax self-attention within each of n_seqs sequences
+ * packed one behind the other: for token i of a sequence
+ *   o_i = sum_j softmax_j(scale q_i . k_j) v_j
+ * over its sequence's tokens j, with causal those up to i; query head h reads
+ * kv head h / (n_heads / n_kv_heads).
+ * Q, K, V  device fp16 or bf16 (dtype) [tokens][ldq / ldk / ldv], head h at columns
+ *          h d .. of a row (so the three parts of a q|k|v linear's output serve
+ *          as they lie); strides % 8 == 0 and at least heads * d; 16-byte aligned
+ * cu_seqlens device int32 [n_seqs + 1], not decreasing: sequence s is rows
+ *          cu_seqlens[s] .. cu_seqlens[s + 1] - 1 (clamped to [0, tokens]); rows
+ *          of no sequence are left as they were, and what they hold is not used
+ * head_dim d: 64, 128 or 256;  n_heads a multiple of n_kv_heads, n_heads <= 65535
+ * scale    > 0, finite
+ * O        device [tokens][ldo] of dtype, ldo % 8 == 0; may not overlap Q, K, V
+ * Probabilities are rounded to dtype for the second product; sums and
+ * statistics are fp32.  Inputs are finite.
+ * Errors: OQ_ERR_NULL, OQ_ERR_SHAPE, OQ_ERR_ALIGN, OQ_ERR_ARG, OQ_ERR_DEVICE,
+ * OQ_ERR_HIP.
+ */
+int oq_attention_prompt(const void* Q, const void* K, const void* V, int64_t tokens, int64_t ldq,
+                        int64_t ldk, int64_t ldv, int32_t dtype, const int32_t* cu_seqlens,
+                        int32_t n_seqs, int32_t n_heads, int32_t n_kv_heads, int32_t head_dim,
+                        int32_t causal, float scale, void* O, int64_t ldo, void* stream);
+
+/* ------------------------------------------------------------------------ */
 /* Static per-step, per-channel activation steps (Section 4.2,               */
 /* eq:perstep_scale with the per-(layer, step, channel) table)               */
 /* ------------------------------------------------------------------------ */
@@ -492,6 +547,108 @@ int oq_quantize_weights_step_host(const double* W_u, int64_t N, int64_t K, int32
  */
 int oq_quantize_weights_step(const void* W_u, int64_t N, int64_t K, int64_t ldw, int32_t had_block,
                              const float* delta, uint8_t* Wq, float* w_scale, void* stream);
+
+/* ------------------------------------------------------------------------ */
+/* Key/value cache in 4 bits (the per-token quantizer of eq:scale, eq:quant   */
+/* on the rows of a backbone's keys and values), and attention over it         */
+/* ------------------------------------------------------------------------ */
+/*
+ * A row is one token and kv head, head_dim channels x.  Its codes are q =
+ * clamp(round_half_even(7 x / max|x|), -7, 7) (formed exactly: a quotient on a
+ * half integer rounds to even, none beside one goes the wrong way), its step
+ * fp32 Delta = max|x| / 7, and the value it stands for q Delta; a row of
+ * zeros has zero codes and step 0.  With rotate_k the keys are rotated first,
+ * x = k H_d / sqrt(d) (d = head_dim, one Hadamard block per head); attention
+ * then rotates its queries alike (q . k is unchanged) and oq_kv4_gather rotates
+ * back.  A rotation of the values folds into the value and output projections.
+ *
+ * All buffers are the caller's.  Pages of page_tokens tokens:
+ *   k_codes [n_pages][n_kv_heads][page_tokens][d / 2]: byte b of a row holds
+ *     channel 2 b in its low nibble and 2 b + 1 in its high one (Xq's packing);
+ *   v_codes [n_pages][n_kv_heads][page_tokens / 16][d / 2][16]: byte (b, t)
+ *     holds channels 2 b and 2 b + 1 of token t of the 16;
+ *   k_scale, v_scale fp32 [n_pages][n_kv_heads][page_tokens].
+ * A slot is page * page_tokens + the token's place in the page.
+ * head_dim 64, 128 or 256; page_tokens a multiple of 32, <= 65536; n_pages >= 1,
+ * < 2^31; n_kv_heads 1 .. 65535; all four pointers 16-byte aligned.
+ */
+typedef struct {
+  uint8_t* k_codes;
+  uint8_t* v_codes;
+  float* k_scale;
+  float* v_scale;
+  int64_t n_pages;
+  int32_t page_tokens;
+  int32_t n_kv_heads;
+  int32_t head_dim;
+  int32_t rotate_k; /* 0 or 1 */
+} oq_kv4_cache;
+
+/*
+ * oq_kv4_append -- quantize n tokens' keys and values into their slots.
+ * K, V     device fp16 or bf16 (dtype) [n][ldk], [n][ldv], head h of a token at
+ *          columns h d .. h d + d - 1; ldk, ldv >= n_kv_heads d, % 8 == 0;
+ *          16-byte aligned
+ * slots    device int64 [n]: slot of each token; a slot below 0 or past the
+ *          cache is skipped (padding tokens).  A slot may occur once in a call;
+ *          of a repeated one the cache holds one of its tokens' bytes each.
+ * Other slots are left as they were.  Input is finite.
+ * Errors: OQ_ERR_NULL, OQ_ERR_SHAPE, OQ_ERR_ALIGN, OQ_ERR_ARG, OQ_ERR_DEVICE,
+ * OQ_ERR_HIP.
+ */
+int oq_kv4_append(const oq_kv4_cache* cache, const void* K, const void* V, int64_t n, int64_t ldk,
+                  int64_t ldv, int32_t dtype, const int64_t* slots, void* stream);
+
+/*
+ * oq_kv4_gather -- the values of n slots as dense rows (fp16, bf16 or fp32 by
+ * dtype): K, V device [n][ldk], [n][ldv], laid out as oq_kv4_append's input;
+ * keys in the basis in which they were appended.  A slot out of range gives
+ * zeros.  For callers that need dense keys and values, as the prefix of
+ * oq_dit_block (P slots give its prefix_k and prefix_v).
+ * Errors: as oq_kv4_append.
+ */
+int oq_kv4_gather(const oq_kv4_cache* cache, const int64_t* slots, int64_t n, void* K, void* V,
+                  int64_t ldk, int64_t ldv, int32_t dtype, void* stream);
+
+/*
+ * oq_attention_kv4 -- softmax attention of packed query tokens over a paged
+ * cache: for sequence b with L = seq_lens[b] cached tokens and n query tokens
+ * i = 0 .. n - 1 (its last n, whose keys are already in the cache),
+ *   o_i = sum_j softmax_j(scale q_i . k_j) v_j,  j < L, and with causal
+ *   j <= L - n + i
+ * per query head; head h reads kv head h / (n_heads / n_kv_heads).  A query that
+ * sees no key gives zeros.  One token per sequence is decoding; several are a
+ * chunk of a prompt or a draft to verify.
+ * Q        device fp16 / bf16 (dtype) [tokens][ldq], head h at columns h d ..;
+ *          ldq >= n_heads d, % 8 == 0, 16-byte aligned.  O likewise (dtype, ldo)
+ * cu_q     device int32 [n_seqs + 1]: sequence b's query tokens are rows
+ *          cu_q[b] .. cu_q[b + 1] - 1; NULL: one each (tokens == n_seqs,
+ *          max_q == 1).  Rows that no sequence has, and those past the first
+ *          max_q of one, are left as they were.
+ * max_q    >= 1, at least the most query tokens of a sequence
+ * block_table  device int32 [n_seqs][table_ld]: page of each page_tokens tokens
+ *          of a sequence; tokens of an entry out of range are masked
+ * seq_lens device int32 [n_seqs]; clamped to [0, max_len]
+ * max_len  >= 0, at least the longest sequence; table_ld page_tokens >= max_len.
+ *          It plans the split over the length: a tight one is faster.
+ * scale    > 0, finite
+ * work     device, 16-byte aligned, at least oq_attention_kv4_workspace_bytes(the
+ *          same sizes) bytes (0: may be NULL), written before it is read;
+ *          calls that share it must not overlap
+ * n_seqs n_kv_heads <= 65535.  Keys, steps and values past a sequence's end are
+ * not used, whatever they hold.  Queries are used as fp16 times a power of two
+ * (rotated ones as two such parts), probabilities as fp16 relative to the
+ * largest contribution, sums and statistics in fp32.
+ * Errors: OQ_ERR_NULL, OQ_ERR_SHAPE, OQ_ERR_ALIGN, OQ_ERR_ARG,
+ * OQ_ERR_WORKSPACE, OQ_ERR_DEVICE, OQ_ERR_HIP.
+ */
+size_t oq_attention_kv4_workspace_bytes(const oq_kv4_cache* cache, int64_t tokens, int32_t n_heads,
+                                        int32_t n_seqs, int32_t max_q, int32_t max_len);
+int oq_attention_kv4(const oq_kv4_cache* cache, const void* Q, int64_t tokens, int64_t ldq,
+                     int32_t n_heads, int32_t dtype, const int32_t* cu_q, int32_t max_q,
+                     const int32_t* block_table, int64_t table_ld, const int32_t* seq_lens,
+                     int32_t n_seqs, int32_t max_len, int32_t causal, float scale, void* O,
+                     int64_t ldo, void* work, size_t work_bytes, void* stream);
 
 /* ------------------------------------------------------------------------ */
 /* DiT denoising-step driver                                                 */

@@ -14,7 +14,7 @@ import torch
 
 from . import _lib
 
-OUT_F16, OUT_BF16 = 0, 1
+OUT_F16, OUT_BF16, OUT_F32 = 0, 1, 2
 
 
 class OQError(RuntimeError):
@@ -288,6 +288,44 @@ def w4a8_gemm_i32(Xq8, Wq, acc=None, stream=None):
     return acc
 
 
+def quantize_weights_i8(W_u, had_block, Wq8=None, w_scale=None, stream=None):
+    """W_u fp16 [N, K] on the device -> (Wq8 int8 [N, K], w_scale f32 [N])."""
+    N, K = W_u.shape
+    if Wq8 is None:
+        Wq8 = torch.empty((N, K), dtype=torch.int8, device=W_u.device)
+    if w_scale is None:
+        w_scale = torch.empty((N,), dtype=torch.float32, device=W_u.device)
+    _check(lib().oq_quantize_weights_i8(_ptr(W_u), N, K, _ld(W_u), had_block, _ptr(Wq8), _ptr(w_scale),
+                                        _stream(stream)), "oq_quantize_weights_i8")
+    return Wq8, w_scale
+
+
+def w8a8_linear(Xq8, x_scale, Wq8, w_scale, bias=None, out_dtype=OUT_F16, Y=None, stream=None):
+    """Y [M, N] = dequant(Xq8 . Wq8^T) with 8-bit codes on both sides (int8 [M, K], [N, K])."""
+    M, K = Xq8.shape
+    N = Wq8.shape[0]
+    if Wq8.shape[1] != K or Xq8.dtype != torch.int8 or Wq8.dtype != torch.int8:
+        raise ValueError("Xq8 and Wq8: int8 [M, K] and [N, K] expected")
+    if Y is None:
+        dt = torch.float16 if out_dtype == OUT_F16 else torch.bfloat16
+        Y = torch.empty((M, N), dtype=dt, device=Xq8.device)
+    _check(lib().oq_w8a8_linear(_ptr(Xq8), _ptr(x_scale), M, _ptr(Wq8), _ptr(w_scale), _ptr(bias), N, K,
+                                _ptr(Y), _ld(Y), out_dtype, _stream(stream)), "oq_w8a8_linear")
+    return Y
+
+
+def w8a8_gemm_i32(Xq8, Wq8, acc=None, stream=None):
+    M, K = Xq8.shape
+    N = Wq8.shape[0]
+    if Wq8.shape[1] != K or Xq8.dtype != torch.int8 or Wq8.dtype != torch.int8:
+        raise ValueError("Xq8 and Wq8: int8 [M, K] and [N, K] expected")
+    if acc is None:
+        acc = torch.empty((M, N), dtype=torch.int32, device=Xq8.device)
+    _check(lib().oq_w8a8_gemm_i32(_ptr(Xq8), M, _ptr(Wq8), N, K, _ptr(acc), _ld(acc), _stream(stream)),
+           "oq_w8a8_gemm_i32")
+    return acc
+
+
 def channel_energy(W, energy=None, stream=None):
     """fp64 [K] column energies sum_n W[n][j]^2 of a device fp16 weight [N, K]."""
     N, K = W.shape
@@ -434,4 +472,6 @@ def quantize_weights_step_host(W_u: np.ndarray, had_block: int, delta: np.ndarra
     return Wq, ws
 
 
+from .attention import (KV4Cache, attention_kv4, attention_kv4_workspace_bytes, attention_prompt,  # noqa: E402,F401
+                        kv4_append, kv4_gather)
 from .dit import DiT  # noqa: E402,F401

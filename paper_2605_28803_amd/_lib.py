@@ -35,6 +35,11 @@ class oq_dit_intermediates(C.Structure):
                                   "x_scale")] + [("codes_tiled", i32)]
 
 
+class oq_kv4_cache(C.Structure):
+    _fields_ = [("k_codes", vp), ("v_codes", vp), ("k_scale", vp), ("v_scale", vp), ("n_pages", i64),
+                ("page_tokens", i32), ("n_kv_heads", i32), ("head_dim", i32), ("rotate_k", i32)]
+
+
 # name -> (restype, argtypes)
 SIGNATURES = {
     "oq_status_string": (C.c_char_p, [i32]),
@@ -70,6 +75,16 @@ SIGNATURES = {
     "oq_rotate_quantize_act_static": (i32, [vp, i64, i64, i64, i32, vp, vp, vp, vp]),
     "oq_rotate_quantize_act_static_tiled": (i32, [vp, i64, i64, i64, i32, vp, vp, vp, vp]),
     "oq_quantize_weights_step_host": (i32, [vp, i64, i64, i32, vp, vp, vp]),
+    "oq_quantize_weights_i8": (i32, [vp, i64, i64, i64, i32, vp, vp, vp]),
+    "oq_w8a8_linear": (i32, [vp, vp, i64, vp, vp, vp, i64, i64, vp, i64, i32, vp]),
+    "oq_w8a8_gemm_i32": (i32, [vp, i64, vp, i64, i64, vp, i64, vp]),
+    "oq_attention_prompt": (i32, [vp, vp, vp, i64, i64, i64, i64, i32, vp, i32, i32, i32, i32, i32, C.c_float, vp, i64,
+                                  vp]),
+    "oq_kv4_append": (i32, [C.POINTER(oq_kv4_cache), vp, vp, i64, i64, i64, i32, vp, vp]),
+    "oq_kv4_gather": (i32, [C.POINTER(oq_kv4_cache), vp, i64, vp, vp, i64, i64, i32, vp]),
+    "oq_attention_kv4_workspace_bytes": (C.c_size_t, [C.POINTER(oq_kv4_cache), i64, i32, i32, i32, i32]),
+    "oq_attention_kv4": (i32, [C.POINTER(oq_kv4_cache), vp, i64, i64, i32, i32, vp, i32, vp, i64, vp, i32, i32, i32,
+                               C.c_float, vp, i64, vp, C.c_size_t, vp]),
     "oq_dit_workspace_bytes": (i32, [C.POINTER(oq_dit_config), C.POINTER(C.c_size_t)]),
     "oq_dit_create": (i32, [C.POINTER(oq_dit_config), C.POINTER(oq_dit_weights), C.POINTER(vp)]),
     "oq_dit_set_workspace": (i32, [vp, vp, C.c_size_t]),

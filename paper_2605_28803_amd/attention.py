@@ -1,0 +1,178 @@
+"""Attention over packed prompts and the 4-bit key/value cache (binding of
+oq_attention_prompt, oq_kv4_* and oq_attention_kv4 in include/oq.h).
+
+Marshalling only.  Shapes, types and devices are checked here, because the C
+entry points see pointers alone.
+"""
+from __future__ import annotations
+
+import ctypes as C
+
+import torch
+
+from . import _lib
+
+_DTYPE = {torch.float16: 0, torch.bfloat16: 1, torch.float32: 2}
+_TORCH = {0: torch.float16, 1: torch.bfloat16, 2: torch.float32}
+
+
+def _want(ok, what):
+    if not ok:
+        raise ValueError(what)
+
+
+def _heads(t, name, head_dim=None):
+    """Token stride of a [tokens, heads, head_dim] tensor whose heads of a token
+    lie side by side."""
+    _want(t.dim() == 3 and (head_dim is None or t.shape[2] == head_dim), f"{name}: [tokens, heads, head_dim] expected")
+    n, h, d = t.shape
+    s0, s1, s2 = t.stride()
+    _want((s2 == 1 or d <= 1) and (s1 == d or h <= 1), f"{name}: the heads of a token must lie side by side")
+    return s0 if n > 1 else h * d
+
+
+def _ints(t, name, dtype, shape, dev):
+    _want(t.dtype == dtype and t.shape == shape and t.is_contiguous() and t.device == dev,
+          f"{name}: contiguous {dtype} {list(shape)} on {dev} expected")
+
+
+def _device(t, *others):
+    """The tensors' device, which has to be the current one (the library
+    launches there)."""
+    dev = t.device
+    _want(dev.type == "cuda" and all(o.device == dev for o in others), "the tensors must be on one GPU")
+    _want(dev.index == torch.cuda.current_device(), f"{dev} is not the current device")
+    return dev
+
+
+def attention_prompt(Q, K, V, cu_seqlens, causal=True, scale=None, O=None, stream=None):
+    """O [T, Hq, d] = softmax(scale Q K^T) V within each packed sequence.
+    Q [T, Hq, d], K, V [T, Hkv, d] fp16 or bf16 (views of a q|k|v output serve),
+    cu_seqlens int32 [n + 1] on the device; scale defaults to d ** -0.5.  Rows of
+    no sequence are left as they were in O (unspecified when O is made here)."""
+    from . import _check, _ptr, _stream
+    ldq, ldk, ldv = _heads(Q, "Q"), _heads(K, "K", Q.shape[2]), _heads(V, "V", Q.shape[2])
+    T, hq, d = Q.shape
+    dev = _device(Q, K, V)
+    _want(K.shape[0] == T and V.shape == K.shape, "K and V need Q's tokens and equal shapes")
+    _want(Q.dtype in _DTYPE and K.dtype == Q.dtype and V.dtype == Q.dtype, "Q, K and V need one type")
+    _ints(cu_seqlens, "cu_seqlens", torch.int32, (max(cu_seqlens.numel(), 1),), dev)
+    if O is None:
+        O = torch.empty((T, hq, d), dtype=Q.dtype, device=dev)
+    _want(O.shape == Q.shape and O.dtype == Q.dtype and O.device == dev, "O: Q's shape, type and device expected")
+    _check(_lib.load().oq_attention_prompt(_ptr(Q), _ptr(K), _ptr(V), T, ldq, ldk, ldv, _DTYPE[Q.dtype], _ptr(cu_seqlens),
+                                           cu_seqlens.numel() - 1, hq, K.shape[1], d, int(causal),
+                                           d ** -0.5 if scale is None else scale, _ptr(O), _heads(O, "O"), _stream(stream)),
+           "oq_attention_prompt")
+    return O
+
+
+class KV4Cache:
+    """The tensors of a paged 4-bit key/value cache (oq_kv4_cache): k_codes
+    uint8 [pages, heads, page_tokens, d / 2], v_codes uint8 [pages, heads,
+    page_tokens / 16, d / 2, 16], k_scale, v_scale fp32 [pages, heads,
+    page_tokens].  KV4Cache.empty makes them."""
+
+    def __init__(self, k_codes, v_codes, k_scale, v_scale, rotate_k=False):
+        _want(k_codes.dim() == 4, "k_codes: [pages, heads, page_tokens, d / 2] expected")
+        p, h, t, half = k_codes.shape
+        dev = k_codes.device
+        for x, name, dtype, shape in ((k_codes, "k_codes", torch.uint8, (p, h, t, half)),
+                                      (v_codes, "v_codes", torch.uint8, (p, h, t // 16, half, 16)),
+                                      (k_scale, "k_scale", torch.float32, (p, h, t)),
+                                      (v_scale, "v_scale", torch.float32, (p, h, t))):
+            _ints(x, name, dtype, shape, dev)
+        self.k_codes, self.v_codes, self.k_scale, self.v_scale = k_codes, v_codes, k_scale, v_scale
+        self.n_pages, self.n_kv_heads, self.page_tokens, self.head_dim = p, h, t, 2 * half
+        self.rotate_k, self.device = bool(rotate_k), dev
+        self._c = _lib.oq_kv4_cache(k_codes.data_ptr(), v_codes.data_ptr(), k_scale.data_ptr(), v_scale.data_ptr(), p, t, h,
+                                    2 * half, int(self.rotate_k))
+        self.ref = C.byref(self._c)
+
+    @classmethod
+    def empty(cls, n_pages, n_kv_heads, head_dim, page_tokens=64, rotate_k=True, device="cuda:0"):
+        """A cache of n_pages pages, cleared."""
+        z = lambda dt, *shape: torch.zeros(shape, dtype=dt, device=device)  # noqa: E731
+        return cls(z(torch.uint8, n_pages, n_kv_heads, page_tokens, head_dim // 2),
+                   z(torch.uint8, n_pages, n_kv_heads, page_tokens // 16, head_dim // 2, 16),
+                   z(torch.float32, n_pages, n_kv_heads, page_tokens), z(torch.float32, n_pages, n_kv_heads, page_tokens),
+                   rotate_k)
+
+
+def kv4_append(cache, K, V, slots, stream=None):
+    """Quantize K, V (fp16 or bf16 [n, Hkv, d]) into the cache's slots (int64
+    [n] = page * page_tokens + place; out of range: skipped)."""
+    from . import _check, _ptr, _stream
+    n = K.shape[0]
+    ldk, ldv = _heads(K, "K", cache.head_dim), _heads(V, "V", cache.head_dim)
+    dev = _device(K, V, cache.k_codes)
+    _want(K.shape[1] == cache.n_kv_heads and V.shape == K.shape, "K and V: [n, the cache's heads, head_dim] expected")
+    _want(K.dtype in _DTYPE and V.dtype == K.dtype, "K and V need one type")
+    _ints(slots, "slots", torch.int64, (n,), dev)
+    _check(_lib.load().oq_kv4_append(cache.ref, _ptr(K), _ptr(V), n, ldk, ldv, _DTYPE[K.dtype], _ptr(slots), _stream(stream)),
+           "oq_kv4_append")
+
+
+def kv4_gather(cache, slots, out_dtype=0, K=None, V=None, stream=None):
+    """(K, V) [n, Hkv, d]: the values that the slots hold (fp16, bf16 or fp32 by
+    out_dtype: OUT_F16, OUT_BF16, OUT_F32)."""
+    from . import _check, _ptr, _stream
+    n = slots.numel()
+    dev = _device(slots, cache.k_codes)
+    _ints(slots, "slots", torch.int64, (n,), dev)
+    shape = (n, cache.n_kv_heads, cache.head_dim)
+    if K is None:
+        K = torch.empty(shape, dtype=_TORCH[out_dtype], device=dev)
+    if V is None:
+        V = torch.empty(shape, dtype=_TORCH[out_dtype], device=dev)
+    for t, name in ((K, "K"), (V, "V")):
+        _want(t.shape == shape and t.dtype == _TORCH.get(out_dtype) and t.device == dev,
+              f"{name}: {list(shape)} of out_dtype on {dev} expected")
+    _check(_lib.load().oq_kv4_gather(cache.ref, _ptr(slots), n, _ptr(K), _ptr(V), _heads(K, "K"), _heads(V, "V"), out_dtype,
+                                     _stream(stream)), "oq_kv4_gather")
+    return K, V
+
+
+def attention_kv4_workspace_bytes(cache, tokens, n_heads, n_seqs, max_q, max_len) -> int:
+    return int(_lib.load().oq_attention_kv4_workspace_bytes(cache.ref, tokens, n_heads, n_seqs, max_q, max_len))
+
+
+def attention_kv4(Q, cache, block_table, seq_lens, cu_q=None, max_q=None, max_len=None, causal=True, scale=None, O=None,
+                  work=None, stream=None):
+    """Attention of query tokens over the cache.  Q fp16 or bf16 [T, Hq, d];
+    block_table int32 [n, width] (pages of each sequence), seq_lens int32 [n].
+    cu_q None: one query token per sequence (T == n); else int32 [n + 1], and
+    max_q (the most query tokens of a sequence) is needed.  max_len (default:
+    what the table's width holds) bounds seq_lens; scale defaults to d ** -0.5.
+    A sequence's query tokens are its last ones (causal).  Rows of no sequence
+    are left as they were in O (unspecified when O is made here)."""
+    from . import _check, _ptr, _stream
+    ldq = _heads(Q, "Q", cache.head_dim)
+    T, hq, d = Q.shape
+    dev = _device(Q, cache.k_codes)
+    n = seq_lens.numel()
+    _want(Q.dtype in _DTYPE, "Q: fp16 or bf16 expected")
+    _want(block_table.dim() == 2, "block_table: [sequences, width] expected")
+    width = block_table.shape[1]
+    _ints(block_table, "block_table", torch.int32, (n, width), dev)
+    _ints(seq_lens, "seq_lens", torch.int32, (n,), dev)
+    if cu_q is None:
+        _want(T == n, "without cu_q there is one query token per sequence")
+        _want(max_q in (None, 1), "without cu_q, max_q is 1")
+        max_q = 1
+    else:
+        _want(max_q is not None, "cu_q needs max_q")
+        _ints(cu_q, "cu_q", torch.int32, (n + 1,), dev)
+    if max_len is None:
+        max_len = min(width * cache.page_tokens, 2 ** 31 - 1)
+    if O is None:
+        O = torch.empty((T, hq, d), dtype=Q.dtype, device=dev)
+    _want(O.shape == Q.shape and O.dtype == Q.dtype and O.device == dev, "O: Q's shape, type and device expected")
+    if work is None:
+        nbytes = attention_kv4_workspace_bytes(cache, T, hq, n, max_q, max_len)
+        work = torch.empty((nbytes,), dtype=torch.uint8, device=dev) if nbytes else None
+    _check(_lib.load().oq_attention_kv4(cache.ref, _ptr(Q), T, ldq, hq, _DTYPE[Q.dtype], _ptr(cu_q), max_q, _ptr(block_table),
+                                        width, _ptr(seq_lens), n, max_len, int(causal), d ** -0.5 if scale is None else scale,
+                                        _ptr(O), _heads(O, "O"), _ptr(work), 0 if work is None else work.numel(),
+                                        _stream(stream)), "oq_attention_kv4")
+    return O

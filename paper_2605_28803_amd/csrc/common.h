@@ -101,7 +101,8 @@ struct GemmArgs {
   const uint16_t* gate;  // EPI_RESID_F32: fp16 [N] per-channel multiplier (null = 1)
   int64_t M, N, K, ldc;
   bool a_tiled;          // A is in the 16-row tiled layout (K % 128 == 0)
-  bool a_i8;             // A holds 8-bit codes, one byte each, [M][K] (W4A8)
+  bool a_i8;             // A holds 8-bit codes, one byte each, [M][K] (W4A8, W8A8)
+  bool b_i8;             // B does too, [N][K] (W8A8; a_i8 is then set)
 };
 
 int gemm_validate(const uint8_t* Xq, int64_t M, const uint8_t* Wq, int64_t N, int64_t K,

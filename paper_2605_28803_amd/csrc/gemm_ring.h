@@ -107,9 +107,13 @@ __device__ __forceinline__ int swz(int row) {
 // per row and stage: a lane reads the 32 bytes that belong to its 16 packed
 // weight bytes and picks their even, then their odd bytes; the products are
 // 16 q wq and the accumulator is shifted by 4.
-template <int EPI, int WM, int WN, int TM, int TN, bool A8, int P, int NS, int KG, int SPREAD>
+// W8: both operands hold 8-bit codes (W8A8), 16 P bytes per row and stage of
+// 16 P codes: nothing is widened, the fragments go to the matrix cores as they
+// lie, one 32-code instruction step per pair of pieces.
+template <int EPI, int WM, int WN, int TM, int TN, bool A8, int P, int NS, int KG, int SPREAD, bool W8 = false>
 __global__ __launch_bounds__(64 * WM * WN * KG, 2)
 void gemm_ring_kernel(GemmArgs a) {
+  static_assert(!(A8 && W8), "A8 is the token operand against packed weights");
   constexpr int NW = WM * WN * KG;
   constexpr int NT = 64 * NW;
   constexpr int BM = 32 * TM * WM, BN = 32 * TN * WN;
@@ -151,9 +155,9 @@ void gemm_ring_kernel(GemmArgs a) {
   ring_tile(static_cast<int>(blockIdx.x), tiles_m, tiles_n, &tm, &tn);
   const int64_t m0 = static_cast<int64_t>(tm) * BM;
   const int64_t n0 = static_cast<int64_t>(tn) * BN;
-  const int64_t Kb = a.K / 2;
+  const int64_t Kb = W8 ? a.K : a.K / 2;
   const int64_t Ka = A8 ? a.K : Kb;
-  const int n64 = static_cast<int>(a.K / 64);          // 64-code pairs
+  const int n64 = static_cast<int>(a.K / (W8 ? 32 : 64));  // pairs of pieces: 64 codes (W8: 32)
   const int nk = (n64 + P / 2 - 1) / (P / 2);          // stages
 
   // 32 x 32 accumulator layout: element e of lane l is row 8 (e / 4) + 4 (l / 32) + e % 4, column l % 32.
@@ -268,7 +272,7 @@ void gemm_ring_kernel(GemmArgs a) {
     for (int j = 0; j < TN; ++j)
       pb[set][j] = *reinterpret_cast<const uint4*>(fB + b * STAGE + j * 32 * P * 16 + ((q ^ sb) * 16));
   };
-  v4i wa[2][TM], wb[2][TN];
+  [[maybe_unused]] v4i wa[2][TM], wb[2][TN];
   // Widen the even (odd = 0) or odd channels of packed set `set` into w*[odd].
   auto widen = [&](int set, int odd, uint32_t mm) {
     constexpr uint32_t m = 0xF0F0F0F0u;
@@ -332,12 +336,14 @@ void gemm_ring_kernel(GemmArgs a) {
   __builtin_amdgcn_s_barrier();
   asm volatile("" ::: "memory");
   read(0, grp, 0);
-  widen(0, 0, grp < n64 ? 0xF0F0F0F0u : 0u);
-  // (Opaque, so that the loop's widening stays where it is written.)
+  if constexpr (!W8) {
+    widen(0, 0, grp < n64 ? 0xF0F0F0F0u : 0u);
+    // (Opaque, so that the loop's widening stays where it is written.)
 #pragma unroll
-  for (int i = 0; i < TM; ++i) asm volatile("" : "+v"(wa[0][i]));
+    for (int i = 0; i < TM; ++i) asm volatile("" : "+v"(wa[0][i]));
 #pragma unroll
-  for (int j = 0; j < TN; ++j) asm volatile("" : "+v"(wb[0][j]));
+    for (int j = 0; j < TN; ++j) asm volatile("" : "+v"(wb[0][j]));
+  }
   int b = 0, bp = NS - 1;
   for (int s = 0; s < nk; ++s) {
     const int bn = b + 1 == NS ? 0 : b + 1;
@@ -354,6 +360,23 @@ void gemm_ring_kernel(GemmArgs a) {
         wait_stage(min(nk - 1 - (s + 1), NS - 2));
         __builtin_amdgcn_s_barrier();
         asm volatile("" ::: "memory");
+      }
+      if constexpr (W8) {
+        // One phase: the next pair is read while this one is multiplied.
+        issue_slot(p + 1 == NP ? s + NS : sprev, p + 1 == NP ? b : bp, std::integral_constant<int, sl>{});
+        issue_slot(p + 1 == NP ? s + NS : sprev, p + 1 == NP ? b : bp, std::integral_constant<int, sl + 1>{});
+        __builtin_amdgcn_sched_barrier(0);
+        if (p + 1 < NP) read(b, grp + (p + 1) * KG, (p + 1) & 1);
+        else read(bn, grp, 0);
+        if (on) {
+#pragma unroll
+          for (int i = 0; i < TM; ++i)
+#pragma unroll
+            for (int j = 0; j < TN; ++j)
+              acc[i][j] = __builtin_amdgcn_mfma_i32_32x32x32_i8(__builtin_bit_cast(v4i, pa[p & 1][i][0]),
+                                                                __builtin_bit_cast(v4i, pb[p & 1][j]), acc[i][j], 0, 0, 0);
+        }
+        return;
       }
       // Phase A: even channels multiplied, odd ones widened, next pair read.
       issue_slot(p + 1 == NP ? s + NS : sprev, p + 1 == NP ? b : bp, std::integral_constant<int, sl>{});
@@ -372,7 +395,7 @@ void gemm_ring_kernel(GemmArgs a) {
     b = bn;
   }
   // Epilogue.
-  constexpr int SH = A8 ? 4 : 8;
+  constexpr int SH = W8 ? 0 : A8 ? 4 : 8;
   const float* sxs = reinterpret_cast<const float*>(smem + LDSB);
   const float* sws = sxs + BM;
   float bias[NC], gate[NC];

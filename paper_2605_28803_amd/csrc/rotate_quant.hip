@@ -343,6 +343,11 @@ extern "C" int oq_rotate_quantize_act_i8(const void* X, int64_t M, int64_t K, in
                        static_cast<hipStream_t>(stream), false, nullptr, false, true);
 }
 
+extern "C" int oq_quantize_weights_i8(const void* W_u, int64_t N, int64_t K, int64_t ldw, int32_t had_block,
+                                      int8_t* Wq8, float* w_scale, void* stream) {
+  return oq_rotate_quantize_act_i8(W_u, N, K, ldw, had_block, nullptr, 0, Wq8, w_scale, stream);
+}
+
 extern "C" int oq_quantize_weights_step(const void* W_u, int64_t N, int64_t K, int64_t ldw, int32_t had_block,
                                         const float* delta, uint8_t* Wq, float* w_scale, void* stream) {
   int st = oq::rq_validate(W_u, N, K, ldw, had_block, Wq, w_scale);

@@ -94,9 +94,12 @@ __device__ __forceinline__ void store_out(const GemmArgs& a, int64_t off, int v,
 
 // A8 (row layout only): 8-bit token codes, 32 bytes per lane and unit,
 // reordered in registers; the accumulator is shifted by 4.
-template <int EPI, int NB, int WAVES, int MB, int UB, bool TILED, bool A8 = false>
+// W8 (with A8): 8-bit weights too; both operands go to the matrix cores in
+// their natural order, 16 bytes per lane and 64-code step.
+template <int EPI, int NB, int WAVES, int MB, int UB, bool TILED, bool A8 = false, bool W8 = false>
 __global__ __launch_bounds__(64 * WAVES) void gemm_small_kernel(GemmArgs a) {
   static_assert(!(A8 && TILED), "8-bit token codes use the row layout");
+  static_assert(A8 || !W8, "8-bit weights take 8-bit token codes");
   constexpr int BNs = 16 * NB, ROWS = 16 * MB, NOUT = ROWS * BNs, NT = 64 * WAVES;
   constexpr int OPT = (NOUT + NT - 1) / NT;  // outputs per thread
   static_assert(NT % BNs == 0, "a thread keeps one output column");
@@ -133,25 +136,29 @@ __global__ __launch_bounds__(64 * WAVES) void gemm_small_kernel(GemmArgs a) {
   }
   const uint8_t* bbase[NB];
 #pragma unroll
-  for (int nb = 0; nb < NB; ++nb) bbase[nb] = a.B + min<int64_t>(n0 + nb * 16 + (lane & 15), a.N - 1) * Kb;
+  for (int nb = 0; nb < NB; ++nb) bbase[nb] = a.B + min<int64_t>(n0 + nb * 16 + (lane & 15), a.N - 1) * Kb * (W8 ? 2 : 1);
   const int piece = 16 * (lane >> 4);  // this lane's 16 bytes of a 64-byte unit (row layout)
 
   // Fragments of UB units starting at u0 (a unit past uend reads unit uend - 1
   // or 0 again; its MFMAs are skipped).
   constexpr int AH = A8 ? 2 : 1;  // 16-byte A loads per unit and row block
-  uint4 fa[UB ? UB : 1][MB][AH], fb[UB ? UB : 1][NB];
+  constexpr int BH = W8 ? 2 : 1;
+  uint4 fa[UB ? UB : 1][MB][AH], fb[UB ? UB : 1][NB][BH];
   auto load_units = [&](int u0) {
 #pragma unroll
     for (int u = 0; u < UB; ++u) {
       const int uu = u0 + u < uend ? u0 + u : max(uend - 1, 0);
 #pragma unroll
-      for (int nb = 0; nb < NB; ++nb) fb[u][nb] = *reinterpret_cast<const uint4*>(bbase[nb] + uu * 64 + piece);
+      for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+        for (int c = 0; c < BH; ++c) fb[u][nb][c] = *reinterpret_cast<const uint4*>(bbase[nb] + uu * 64 * BH + piece + 64 * c);
 #pragma unroll
       for (int rb = 0; rb < MB; ++rb)
 #pragma unroll
         for (int c = 0; c < AH; ++c)
           fa[u][rb][c] = *reinterpret_cast<const uint4*>(
               TILED ? abase[rb] + static_cast<int64_t>(uu) * 1024
+              : W8 ? abase[rb] + uu * 128 + piece + 64 * c
                     : abase[rb] + uu * 64 * AH + piece * AH + 16 * c);
     }
   };
@@ -197,12 +204,17 @@ __global__ __launch_bounds__(64 * WAVES) void gemm_small_kernel(GemmArgs a) {
         for (int h = 0; h < 2; ++h) {
           v4i wb[NB];
 #pragma unroll
-          for (int nb = 0; nb < NB; ++nb)
-            wb[nb] = widen16_u2(h ? make_uint2(fb[u][nb].z, fb[u][nb].w) : make_uint2(fb[u][nb].x, fb[u][nb].y));
+          for (int nb = 0; nb < NB; ++nb) {
+            const uint4 pb = fb[u][nb][W8 ? h : 0];
+            if constexpr (W8) wb[nb] = __builtin_bit_cast(v4i, pb);
+            else wb[nb] = widen16_u2(h ? make_uint2(pb.z, pb.w) : make_uint2(pb.x, pb.y));
+          }
 #pragma unroll
           for (int rb = 0; rb < MB; ++rb) {
             v4i xa;
-            if constexpr (A8) {
+            if constexpr (W8) {
+              xa = __builtin_bit_cast(v4i, aok[rb] ? fa[u][rb][h] : make_uint4(0, 0, 0, 0));
+            } else if constexpr (A8) {
               xa = order16_i8(aok[rb] ? fa[u][rb][h] : make_uint4(0, 0, 0, 0));
             } else {
               const uint2 pa = h ? make_uint2(fa[u][rb][0].z, fa[u][rb][0].w) : make_uint2(fa[u][rb][0].x, fa[u][rb][0].y);
@@ -230,11 +242,16 @@ __global__ __launch_bounds__(64 * WAVES) void gemm_small_kernel(GemmArgs a) {
     const int64_t off = static_cast<int64_t>(nu) * 64 + 8 * (lane >> 4);
     v4i wb[NB];
 #pragma unroll
-    for (int nb = 0; nb < NB; ++nb) wb[nb] = widen16_u2(*reinterpret_cast<const uint2*>(bbase[nb] + off));
+    for (int nb = 0; nb < NB; ++nb) {
+      if constexpr (W8) wb[nb] = __builtin_bit_cast(v4i, *reinterpret_cast<const uint4*>(bbase[nb] + 2 * off));
+      else wb[nb] = widen16_u2(*reinterpret_cast<const uint2*>(bbase[nb] + off));
+    }
 #pragma unroll
     for (int rb = 0; rb < MB; ++rb) {
       v4i xa;
-      if constexpr (A8)
+      if constexpr (W8)
+        xa = __builtin_bit_cast(v4i, aok[rb] ? *reinterpret_cast<const uint4*>(abase[rb] + 2 * off) : make_uint4(0, 0, 0, 0));
+      else if constexpr (A8)
         xa = order16_i8(aok[rb] ? *reinterpret_cast<const uint4*>(abase[rb] + 2 * off) : make_uint4(0, 0, 0, 0));
       else
         xa = widen16_u2(aok[rb] ? *reinterpret_cast<const uint2*>(abase[rb] + off) : make_uint2(0, 0));
@@ -261,11 +278,11 @@ __global__ __launch_bounds__(64 * WAVES) void gemm_small_kernel(GemmArgs a) {
     int sum = 0;
 #pragma unroll
     for (int w = 0; w < WAVES; ++w) sum += red[w][i];
-    store_out<EPI>(a, gr * a.ldc + egc, sum >> (A8 ? 4 : 8), e_xs[u], e_ws, e_bias, e_gate, e_res[u]);
+    store_out<EPI>(a, gr * a.ldc + egc, sum >> (W8 ? 0 : A8 ? 4 : 8), e_xs[u], e_ws, e_bias, e_gate, e_res[u]);
   }
 }
 
-template <int EPI, bool TILED, int MB, bool A8 = false>
+template <int EPI, bool TILED, int MB, bool A8 = false, bool W8 = false>
 int launch_small_mb(const GemmArgs& a, hipStream_t stream) {
   const SmallShape sh = small_shape(a.N, a.K, A8);
   const int bn = 16 * sh.nb;
@@ -273,7 +290,7 @@ int launch_small_mb(const GemmArgs& a, hipStream_t stream) {
   const dim3 block(64 * sh.waves);
 #define OQ_SMALL(NB, WV, UB)                                                                             \
   if (sh.nb == NB && sh.waves == WV && sh.ub == UB) {                                                    \
-    hipLaunchKernelGGL((gemm_small_kernel<EPI, NB, WV, MB, UB, TILED, A8>), grid, block, 0, stream, a);  \
+    hipLaunchKernelGGL((gemm_small_kernel<EPI, NB, WV, MB, UB, TILED, A8, W8>), grid, block, 0, stream, a);  \
     return launch_status();                                                                              \
   }
   if constexpr (!TILED) {  // (the tiled layout has K % 128 == 0)
@@ -311,6 +328,12 @@ int launch_small(const GemmArgs& a, hipStream_t stream) {
 
 template <int EPI>
 int launch_small_any(const GemmArgs& a, hipStream_t stream) {
+  if (a.b_i8) {
+    if constexpr (EPI == EPI_RESID_F32 || EPI == EPI_GELU_F16) return OQ_ERR_ARG;  // DiT paths only
+    else
+      return a.M <= 16 ? launch_small_mb<EPI, false, 1, true, true>(a, stream)
+                       : launch_small_mb<EPI, false, 4, true, true>(a, stream);
+  }
   if (a.a_i8)
     return a.M <= 16 ? launch_small_mb<EPI, false, 1, true>(a, stream) : launch_small_mb<EPI, false, 4, true>(a, stream);
   return a.a_tiled ? launch_small<EPI, true>(a, stream) : launch_small<EPI, false>(a, stream);
@@ -328,22 +351,22 @@ int gemm_validate(const uint8_t* Xq, int64_t M, const uint8_t* Wq, int64_t N, in
   return OQ_OK;
 }
 
-template <int WM, int WN, int TM, int TN, bool A8, int P, int NS, int KG, int SPREAD>
+template <int WM, int WN, int TM, int TN, bool A8, int P, int NS, int KG, int SPREAD, bool W8 = false>
 int launch_ring(const GemmArgs& a, Epilogue epi, hipStream_t stream) {
   constexpr int BM = 32 * TM * WM, BN = 32 * TN * WN;
   const int64_t tiles = ((a.M + BM - 1) / BM) * ((a.N + BN - 1) / BN);
   const dim3 g(static_cast<unsigned>(tiles)), b(64 * WM * WN * KG);
-#define OQ_RING(E) hipLaunchKernelGGL((gemm_ring_kernel<E, WM, WN, TM, TN, A8, P, NS, KG, SPREAD>), g, b, 0, stream, a)
+#define OQ_RING(E) hipLaunchKernelGGL((gemm_ring_kernel<E, WM, WN, TM, TN, A8, P, NS, KG, SPREAD, W8>), g, b, 0, stream, a)
   switch (epi) {
     case EPI_I32: OQ_RING(EPI_I32); break;
     case EPI_F16: OQ_RING(EPI_F16); break;
     case EPI_BF16: OQ_RING(EPI_BF16); break;
     case EPI_GELU_F16:
-      if constexpr (A8) return OQ_ERR_ARG;  // a DiT path only
+      if constexpr (A8 || W8) return OQ_ERR_ARG;  // a DiT path only
       else OQ_RING(EPI_GELU_F16);
       break;
     case EPI_RESID_F32:
-      if constexpr (A8) return OQ_ERR_ARG;  // the residual epilogue is a W4A4 DiT path only
+      if constexpr (A8 || W8) return OQ_ERR_ARG;  // the residual epilogue is a W4A4 DiT path only
       else OQ_RING(EPI_RESID_F32);
       break;
     default: return OQ_ERR_ARG;
@@ -363,6 +386,13 @@ int gemm_launch(const GemmArgs& a, Epilogue epi, hipStream_t stream) {
       case EPI_RESID_F32: return launch_small_any<EPI_RESID_F32>(a, stream);
       case EPI_GELU_F16: return launch_small_any<EPI_GELU_F16>(a, stream);
       default: return OQ_ERR_ARG;
+    }
+  }
+  if (a.b_i8) {
+    switch (ring_tiling(a.M, a.N, a.K, true)) {
+      case 0: return launch_ring<2, 4, 4, 2, false, 8, 2, 1, 4, true>(a, epi, stream);
+      case 1: return launch_ring<2, 2, 2, 2, false, 8, 2, 1, 1, true>(a, epi, stream);
+      default: return launch_ring<1, 2, 2, 1, false, 8, 2, 2, 1, true>(a, epi, stream);
     }
   }
   if (a.a_i8) {
@@ -454,5 +484,31 @@ extern "C" int oq_w4a8_gemm_i32(const int8_t* Xq8, int64_t M, const uint8_t* Wq,
   if (st != OQ_OK || M == 0) return st;
   if ((st = oq::device_check()) != OQ_OK) return st;
   oq::GemmArgs a{A, Wq, nullptr, nullptr, nullptr, acc, nullptr, M, N, K, ldc, false, true};
+  return oq::gemm_launch(a, oq::EPI_I32, static_cast<hipStream_t>(stream));
+}
+
+extern "C" int oq_w8a8_linear(const int8_t* Xq8, const float* x_scale, int64_t M, const int8_t* Wq8,
+                              const float* w_scale, const void* bias, int64_t N, int64_t K, void* Y,
+                              int64_t ldy, int32_t out_dtype, void* stream) {
+  const uint8_t* A = reinterpret_cast<const uint8_t*>(Xq8);
+  const uint8_t* B = reinterpret_cast<const uint8_t*>(Wq8);
+  int st = oq::gemm_validate(A, M, B, N, K, Y, ldy, 8);
+  if (st != OQ_OK || M == 0) return st;
+  if (!x_scale || !w_scale) return OQ_ERR_NULL;
+  if (out_dtype != OQ_OUT_F16 && out_dtype != OQ_OUT_BF16) return OQ_ERR_ARG;
+  if (!oq::aligned(x_scale, 4) || !oq::aligned(w_scale, 4) || (bias && !oq::aligned(bias, 2))) return OQ_ERR_ALIGN;
+  if ((st = oq::device_check()) != OQ_OK) return st;
+  oq::GemmArgs a{A, B, x_scale, w_scale, static_cast<const uint16_t*>(bias), Y, nullptr, M, N, K, ldy, false, true, true};
+  return oq::gemm_launch(a, out_dtype == OQ_OUT_F16 ? oq::EPI_F16 : oq::EPI_BF16, static_cast<hipStream_t>(stream));
+}
+
+extern "C" int oq_w8a8_gemm_i32(const int8_t* Xq8, int64_t M, const int8_t* Wq8, int64_t N, int64_t K, int32_t* acc,
+                                int64_t ldc, void* stream) {
+  const uint8_t* A = reinterpret_cast<const uint8_t*>(Xq8);
+  const uint8_t* B = reinterpret_cast<const uint8_t*>(Wq8);
+  int st = oq::gemm_validate(A, M, B, N, K, acc, ldc, 4);
+  if (st != OQ_OK || M == 0) return st;
+  if ((st = oq::device_check()) != OQ_OK) return st;
+  oq::GemmArgs a{A, B, nullptr, nullptr, nullptr, acc, nullptr, M, N, K, ldc, false, true, true};
   return oq::gemm_launch(a, oq::EPI_I32, static_cast<hipStream_t>(stream));
 }

@@ -64,6 +64,7 @@ class DiT:
         self.s_table = np.ascontiguousarray(inp["s_table"], dtype=np.float32)
         blocks = (_lib.oq_dit_block * L)()
         self.qweights = []
+        self._prefix = []  # pi: (K, V) [B, P, D] of each block
         null = _lib.oq_qweight(None, None)
         for l in range(L):
             bw = w["blocks"][l]
@@ -87,8 +88,8 @@ class DiT:
             else:
                 g2 = h16(bw["g2"])
                 kp, vp = h16(inp["kp"][l]), h16(inp["vp"][l])
-                for t_ in (g2, kp, vp):
-                    keep(t_)
+                keep(g2)
+                self._prefix.append((kp, vp))
                 blocks[l] = _lib.oq_dit_block(g1.data_ptr(), g2.data_ptr(), qw("wqkv"), qw("wo"), qw("wgu"),
                                               qw("wd"), kp.data_ptr(), vp.data_ptr(), None, null)
         self._blocks = blocks
@@ -115,6 +116,20 @@ class DiT:
         from . import _check
         _check(self.lib.oq_dit_set_condition(self.handle, cond.data_ptr(), self._stream(stream)),
                "oq_dit_set_condition")
+
+    def load_prefix(self, l, cache, slots, stream=None):
+        """pi: refill the prefix keys and values of block l from a 4-bit cache
+        (KV4Cache with the head's n_heads and head_dim) that a backbone filled;
+        slots int64 [B * P] on the device.  In place: captured steps use it from
+        their next replay on."""
+        from . import OUT_F16, kv4_gather
+        if not self._prefix:
+            raise ValueError("only a pi handle has prefix keys and values")
+        H, hd = self.cfg_c.n_heads, self.cfg_c.head_dim
+        if (cache.n_kv_heads, cache.head_dim) != (H, hd):
+            raise ValueError(f"the cache needs {H} heads of {hd} channels")
+        K, V = (t.view(-1, H, hd) for t in self._prefix[l])
+        kv4_gather(cache, slots, OUT_F16, K=K, V=V, stream=stream)
 
     def _stream(self, stream):
         s = torch.cuda.current_stream(self.device) if stream is None else stream
