@@ -569,7 +569,7 @@ int oq_quantize_weights_step(const void* W_u, int64_t N, int64_t K, int64_t ldw,
  *     holds channels 2 b and 2 b + 1 of token t of the 16;
  *   k_scale, v_scale fp32 [n_pages][n_kv_heads][page_tokens].
  * A slot is page * page_tokens + the token's place in the page.
- * head_dim 64, 128 or 256; page_tokens a multiple of 32, <= 65536; n_pages >= 1,
+ * head_dim 64, 128 or 256; page_tokens a multiple of 16, <= 65536; n_pages >= 1,
  * < 2^31; n_kv_heads 1 .. 65535; all four pointers 16-byte aligned.
  */
 typedef struct {
@@ -625,7 +625,7 @@ int oq_kv4_gather(const oq_kv4_cache* cache, const int64_t* slots, int64_t n, vo
  *          cu_q[b] .. cu_q[b + 1] - 1; NULL: one each (tokens == n_seqs,
  *          max_q == 1).  Rows that no sequence has, and those past the first
  *          max_q of one, are left as they were.
- * max_q    >= 1, at least the most query tokens of a sequence
+ * max_q    1 .. 65535, at least the most query tokens of a sequence
  * block_table  device int32 [n_seqs][table_ld]: page of each page_tokens tokens
  *          of a sequence; tokens of an entry out of range are masked
  * seq_lens device int32 [n_seqs]; clamped to [0, max_len]

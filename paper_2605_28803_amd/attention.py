@@ -10,7 +10,7 @@ import ctypes as C
 
 import torch
 
-from . import _lib
+from . import _check, _lib, _ptr, _stream  # (the package has these before it imports this module)
 
 _DTYPE = {torch.float16: 0, torch.bfloat16: 1, torch.float32: 2}
 _TORCH = {0: torch.float16, 1: torch.bfloat16, 2: torch.float32}
@@ -21,27 +21,30 @@ def _want(ok, what):
         raise ValueError(what)
 
 
+# The host's time bounds the smallest calls, so the checks below ask a tensor as little as they can.
+
 def _heads(t, name, head_dim=None):
     """Token stride of a [tokens, heads, head_dim] tensor whose heads of a token
     lie side by side."""
-    _want(t.dim() == 3 and (head_dim is None or t.shape[2] == head_dim), f"{name}: [tokens, heads, head_dim] expected")
+    _want(t.dim() == 3, f"{name}: [tokens, heads, head_dim] expected")
     n, h, d = t.shape
+    _want(head_dim is None or d == head_dim, f"{name}: [tokens, heads, head_dim] expected")
     s0, s1, s2 = t.stride()
     _want((s2 == 1 or d <= 1) and (s1 == d or h <= 1), f"{name}: the heads of a token must lie side by side")
     return s0 if n > 1 else h * d
 
 
-def _ints(t, name, dtype, shape, dev):
-    _want(t.dtype == dtype and t.shape == shape and t.is_contiguous() and t.device == dev,
-          f"{name}: contiguous {dtype} {list(shape)} on {dev} expected")
+def _ints(t, name, dtype, n, dev):
+    if t.dtype is not dtype or t.numel() != n or not t.is_contiguous() or t.get_device() != dev:
+        raise ValueError(f"{name}: contiguous {dtype} of {n} elements on cuda:{dev} expected")
 
 
 def _device(t, *others):
-    """The tensors' device, which has to be the current one (the library
+    """Index of the tensors' device, which has to be the current one (the library
     launches there)."""
-    dev = t.device
-    _want(dev.type == "cuda" and all(o.device == dev for o in others), "the tensors must be on one GPU")
-    _want(dev.index == torch.cuda.current_device(), f"{dev} is not the current device")
+    dev = t.get_device()
+    _want(dev >= 0 and all(o.get_device() == dev for o in others), "the tensors must be on one GPU")
+    _want(dev == torch.cuda.current_device(), f"cuda:{dev} is not the current device")
     return dev
 
 
@@ -50,19 +53,22 @@ def attention_prompt(Q, K, V, cu_seqlens, causal=True, scale=None, O=None, strea
     Q [T, Hq, d], K, V [T, Hkv, d] fp16 or bf16 (views of a q|k|v output serve),
     cu_seqlens int32 [n + 1] on the device; scale defaults to d ** -0.5.  Rows of
     no sequence are left as they were in O (unspecified when O is made here)."""
-    from . import _check, _ptr, _stream
     ldq, ldk, ldv = _heads(Q, "Q"), _heads(K, "K", Q.shape[2]), _heads(V, "V", Q.shape[2])
     T, hq, d = Q.shape
     dev = _device(Q, K, V)
     _want(K.shape[0] == T and V.shape == K.shape, "K and V need Q's tokens and equal shapes")
     _want(Q.dtype in _DTYPE and K.dtype == Q.dtype and V.dtype == Q.dtype, "Q, K and V need one type")
-    _ints(cu_seqlens, "cu_seqlens", torch.int32, (max(cu_seqlens.numel(), 1),), dev)
+    n_cu = cu_seqlens.numel()
+    _want(n_cu >= 1, "cu_seqlens: at least one element expected")
+    _ints(cu_seqlens, "cu_seqlens", torch.int32, n_cu, dev)
     if O is None:
-        O = torch.empty((T, hq, d), dtype=Q.dtype, device=dev)
-    _want(O.shape == Q.shape and O.dtype == Q.dtype and O.device == dev, "O: Q's shape, type and device expected")
+        O, ldo = torch.empty((T, hq, d), dtype=Q.dtype, device=Q.device), hq * d
+    else:
+        _want(O.shape == Q.shape and O.dtype == Q.dtype and O.get_device() == dev, "O: Q's shape, type and device expected")
+        ldo = _heads(O, "O")
     _check(_lib.load().oq_attention_prompt(_ptr(Q), _ptr(K), _ptr(V), T, ldq, ldk, ldv, _DTYPE[Q.dtype], _ptr(cu_seqlens),
-                                           cu_seqlens.numel() - 1, hq, K.shape[1], d, int(causal),
-                                           d ** -0.5 if scale is None else scale, _ptr(O), _heads(O, "O"), _stream(stream)),
+                                           n_cu - 1, hq, K.shape[1], d, int(causal),
+                                           d ** -0.5 if scale is None else scale, _ptr(O), ldo, _stream(stream)),
            "oq_attention_prompt")
     return O
 
@@ -81,7 +87,8 @@ class KV4Cache:
                                       (v_codes, "v_codes", torch.uint8, (p, h, t // 16, half, 16)),
                                       (k_scale, "k_scale", torch.float32, (p, h, t)),
                                       (v_scale, "v_scale", torch.float32, (p, h, t))):
-            _ints(x, name, dtype, shape, dev)
+            _want(x.dtype == dtype and x.shape == shape and x.is_contiguous() and x.device == dev,
+                  f"{name}: contiguous {dtype} {list(shape)} on {dev} expected")
         self.k_codes, self.v_codes, self.k_scale, self.v_scale = k_codes, v_codes, k_scale, v_scale
         self.n_pages, self.n_kv_heads, self.page_tokens, self.head_dim = p, h, t, 2 * half
         self.rotate_k, self.device = bool(rotate_k), dev
@@ -102,13 +109,12 @@ class KV4Cache:
 def kv4_append(cache, K, V, slots, stream=None):
     """Quantize K, V (fp16 or bf16 [n, Hkv, d]) into the cache's slots (int64
     [n] = page * page_tokens + place; out of range: skipped)."""
-    from . import _check, _ptr, _stream
     n = K.shape[0]
     ldk, ldv = _heads(K, "K", cache.head_dim), _heads(V, "V", cache.head_dim)
     dev = _device(K, V, cache.k_codes)
     _want(K.shape[1] == cache.n_kv_heads and V.shape == K.shape, "K and V: [n, the cache's heads, head_dim] expected")
     _want(K.dtype in _DTYPE and V.dtype == K.dtype, "K and V need one type")
-    _ints(slots, "slots", torch.int64, (n,), dev)
+    _ints(slots, "slots", torch.int64, n, dev)
     _check(_lib.load().oq_kv4_append(cache.ref, _ptr(K), _ptr(V), n, ldk, ldv, _DTYPE[K.dtype], _ptr(slots), _stream(stream)),
            "oq_kv4_append")
 
@@ -116,19 +122,22 @@ def kv4_append(cache, K, V, slots, stream=None):
 def kv4_gather(cache, slots, out_dtype=0, K=None, V=None, stream=None):
     """(K, V) [n, Hkv, d]: the values that the slots hold (fp16, bf16 or fp32 by
     out_dtype: OUT_F16, OUT_BF16, OUT_F32)."""
-    from . import _check, _ptr, _stream
     n = slots.numel()
     dev = _device(slots, cache.k_codes)
-    _ints(slots, "slots", torch.int64, (n,), dev)
+    _ints(slots, "slots", torch.int64, n, dev)
+    dt = _TORCH.get(out_dtype)
+    _want(dt is not None, "out_dtype: OUT_F16, OUT_BF16 or OUT_F32 expected")
     shape = (n, cache.n_kv_heads, cache.head_dim)
-    if K is None:
-        K = torch.empty(shape, dtype=_TORCH[out_dtype], device=dev)
-    if V is None:
-        V = torch.empty(shape, dtype=_TORCH[out_dtype], device=dev)
+    ld = []
     for t, name in ((K, "K"), (V, "V")):
-        _want(t.shape == shape and t.dtype == _TORCH.get(out_dtype) and t.device == dev,
-              f"{name}: {list(shape)} of out_dtype on {dev} expected")
-    _check(_lib.load().oq_kv4_gather(cache.ref, _ptr(slots), n, _ptr(K), _ptr(V), _heads(K, "K"), _heads(V, "V"), out_dtype,
+        if t is None:
+            ld.append(shape[1] * shape[2])
+        else:
+            _want(t.shape == shape and t.dtype == dt and t.get_device() == dev, f"{name}: {list(shape)} of {dt} on cuda:{dev} expected")
+            ld.append(_heads(t, name))
+    K = torch.empty(shape, dtype=dt, device=slots.device) if K is None else K
+    V = torch.empty(shape, dtype=dt, device=slots.device) if V is None else V
+    _check(_lib.load().oq_kv4_gather(cache.ref, _ptr(slots), n, _ptr(K), _ptr(V), ld[0], ld[1], out_dtype,
                                      _stream(stream)), "oq_kv4_gather")
     return K, V
 
@@ -146,33 +155,36 @@ def attention_kv4(Q, cache, block_table, seq_lens, cu_q=None, max_q=None, max_le
     what the table's width holds) bounds seq_lens; scale defaults to d ** -0.5.
     A sequence's query tokens are its last ones (causal).  Rows of no sequence
     are left as they were in O (unspecified when O is made here)."""
-    from . import _check, _ptr, _stream
     ldq = _heads(Q, "Q", cache.head_dim)
     T, hq, d = Q.shape
     dev = _device(Q, cache.k_codes)
     n = seq_lens.numel()
     _want(Q.dtype in _DTYPE, "Q: fp16 or bf16 expected")
-    _want(block_table.dim() == 2, "block_table: [sequences, width] expected")
+    _want(block_table.dim() == 2 and block_table.shape[0] == n, "block_table: [sequences, width] expected")
     width = block_table.shape[1]
-    _ints(block_table, "block_table", torch.int32, (n, width), dev)
-    _ints(seq_lens, "seq_lens", torch.int32, (n,), dev)
+    _ints(block_table, "block_table", torch.int32, n * width, dev)
+    _ints(seq_lens, "seq_lens", torch.int32, n, dev)
     if cu_q is None:
         _want(T == n, "without cu_q there is one query token per sequence")
         _want(max_q in (None, 1), "without cu_q, max_q is 1")
         max_q = 1
     else:
         _want(max_q is not None, "cu_q needs max_q")
-        _ints(cu_q, "cu_q", torch.int32, (n + 1,), dev)
+        _ints(cu_q, "cu_q", torch.int32, n + 1, dev)
     if max_len is None:
         max_len = min(width * cache.page_tokens, 2 ** 31 - 1)
     if O is None:
-        O = torch.empty((T, hq, d), dtype=Q.dtype, device=dev)
-    _want(O.shape == Q.shape and O.dtype == Q.dtype and O.device == dev, "O: Q's shape, type and device expected")
+        O, ldo = torch.empty((T, hq, d), dtype=Q.dtype, device=Q.device), hq * d
+    else:
+        _want(O.shape == Q.shape and O.dtype == Q.dtype and O.get_device() == dev, "O: Q's shape, type and device expected")
+        ldo = _heads(O, "O")
     if work is None:
         nbytes = attention_kv4_workspace_bytes(cache, T, hq, n, max_q, max_len)
-        work = torch.empty((nbytes,), dtype=torch.uint8, device=dev) if nbytes else None
+        work = torch.empty((nbytes,), dtype=torch.uint8, device=Q.device) if nbytes else None
+    else:
+        _want(work.get_device() == dev and work.is_contiguous() and work.element_size() == 1, "work: contiguous bytes on Q's device expected")
     _check(_lib.load().oq_attention_kv4(cache.ref, _ptr(Q), T, ldq, hq, _DTYPE[Q.dtype], _ptr(cu_q), max_q, _ptr(block_table),
                                         width, _ptr(seq_lens), n, max_len, int(causal), d ** -0.5 if scale is None else scale,
-                                        _ptr(O), _heads(O, "O"), _ptr(work), 0 if work is None else work.numel(),
+                                        _ptr(O), ldo, _ptr(work), 0 if work is None else work.numel(),
                                         _stream(stream)), "oq_attention_kv4")
     return O

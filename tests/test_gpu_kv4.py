@@ -40,7 +40,7 @@ def _same(cache, bufs):
 
 @pytest.mark.parametrize("dtype", [torch.float16, torch.bfloat16])
 @pytest.mark.parametrize("rotate", [False, True])
-@pytest.mark.parametrize("d,hk,page", [(64, 3, 32), (128, 2, 96), (256, 1, 64), (128, 8, 256)])
+@pytest.mark.parametrize("d,hk,page", [(64, 3, 16), (64, 3, 32), (128, 2, 96), (256, 1, 64), (128, 8, 256)])
 def test_append_and_gather(d, hk, page, rotate, dtype):
     g = _gen(d + hk)
     pages, n = 5, 2 * page + 13
@@ -194,7 +194,7 @@ def _attention(lens, nqs, hq, hk, d, page, rotate, causal, dtype, max_len=None, 
 
 @pytest.mark.parametrize("dtype", [torch.float16, torch.bfloat16])
 @pytest.mark.parametrize("rotate", [False, True])
-@pytest.mark.parametrize("d,hq,hk,page", [(64, 4, 4, 32), (128, 8, 2, 64), (256, 8, 1, 96), (128, 15, 3, 128)])
+@pytest.mark.parametrize("d,hq,hk,page", [(64, 4, 4, 16), (64, 12, 2, 48), (128, 8, 2, 64), (256, 8, 1, 96), (128, 15, 3, 128)])
 def test_one_token_each(d, hq, hk, page, rotate, dtype):
     lens = [1, 0, 33, 127, 128, 129, 300, 2]
     _attention(lens, [1] * len(lens), hq, hk, d, page, rotate, True, dtype, cu=False)

@@ -28,8 +28,8 @@ def _c(**kw):
 
 
 BAD_CACHES = [(dict(k_codes=None), NULL), (dict(v_scale=None), NULL), (dict(head_dim=96), SHAPE), (dict(head_dim=0), SHAPE),
-              (dict(n_pages=0), SHAPE), (dict(n_pages=2 ** 31), SHAPE), (dict(page_tokens=16), SHAPE), (dict(page_tokens=48), SHAPE),
-              (dict(page_tokens=65568), SHAPE), (dict(n_kv_heads=0), SHAPE), (dict(n_kv_heads=65536), SHAPE),
+              (dict(n_pages=0), SHAPE), (dict(n_pages=2 ** 31), SHAPE), (dict(page_tokens=8), SHAPE), (dict(page_tokens=56), SHAPE),
+              (dict(page_tokens=65552), SHAPE), (dict(n_pages=2 ** 30, page_tokens=65536), SHAPE), (dict(n_kv_heads=0), SHAPE), (dict(n_kv_heads=65536), SHAPE),
               (dict(k_codes=0x10004), ALIGN), (dict(k_scale=0x10008), ALIGN), (dict(rotate_k=2), ARG)]
 
 
@@ -75,7 +75,7 @@ def _attend(lib, cache=None, Q=P16, tokens=4, ldq=1024, heads=8, dtype=0, cu=Non
     (dict(Q=None), NULL), (dict(O=None), NULL), (dict(lens=None), NULL), (dict(table=None), NULL),
     (dict(Q=P4), ALIGN), (dict(O=P4), ALIGN), (dict(work=P4), ALIGN), (dict(lens=P2), ALIGN), (dict(table=P2), ALIGN),
     (dict(cu=P2), ALIGN), (dict(ldq=1028), ALIGN), (dict(ldo=1028), ALIGN),
-    (dict(tokens=-1), SHAPE), (dict(tokens=5), SHAPE), (dict(max_q=2), SHAPE), (dict(max_q=0), SHAPE), (dict(heads=7), SHAPE),
+    (dict(tokens=-1), SHAPE), (dict(tokens=5), SHAPE), (dict(max_q=2), SHAPE), (dict(max_q=0), SHAPE), (dict(max_q=65536, cu=P16), SHAPE), (dict(heads=7), SHAPE),
     (dict(heads=0), SHAPE), (dict(n=-1), SHAPE), (dict(n=40000, tokens=40000), SHAPE), (dict(max_len=-1), SHAPE),
     (dict(max_len=513), SHAPE), (dict(table_ld=-1), SHAPE), (dict(ldq=1016), SHAPE), (dict(ldo=8), SHAPE),
     (dict(dtype=2), ARG), (dict(dtype=-1), ARG), (dict(causal=2), ARG), (dict(scale=0.0), ARG), (dict(scale=-1.0), ARG),
