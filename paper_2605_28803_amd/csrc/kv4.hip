@@ -35,7 +35,8 @@ struct Cache {
   float* ks;
   float* vs;
   int64_t n_slots;  // n_pages * page_tokens
-  int page, hk;
+  int hk;
+  uint32_t p16, p16_inv;  // 16-token blocks of a page, and floor(2^32 / p16) (p16 = 1: 2^32 - 1)
 };
 
 template <bool BF>
@@ -62,6 +63,29 @@ __device__ __forceinline__ void store8(uint16_t* p, const float (&y)[8]) {
   *reinterpret_cast<uint4*>(p) = make_uint4(pack2<BF>(y[0], y[1]), pack2<BF>(y[2], y[3]), pack2<BF>(y[4], y[5]), pack2<BF>(y[6], y[7]));
 }
 
+// Value of lane ^ H (H < 32) on the vector unit.
+template <int H>
+__device__ __forceinline__ float lane_swap(float v) {
+  if constexpr (H <= 2) return rqd::lane_xor<H>(v);
+  else if constexpr (H <= 8) return rqd::lane_xor_dpp<H>(v);
+  else return lane_xor_far<H>(v);
+}
+template <int H>
+__device__ __forceinline__ double lane_swap(double v) {
+  const uint64_t b = __builtin_bit_cast(uint64_t, v);
+  const float lo = lane_swap<H>(__uint_as_float(static_cast<uint32_t>(b)));
+  const float hi = lane_swap<H>(__uint_as_float(static_cast<uint32_t>(b >> 32)));
+  return __builtin_bit_cast(double, static_cast<uint64_t>(__float_as_uint(hi)) << 32 | __float_as_uint(lo));
+}
+// f(H) for the lane bits H = 1, 2 .. LR / 2 of a row of LR lanes.
+template <int LR, int H = 1, typename F>
+__device__ __forceinline__ void over_lanes(F&& f) {
+  if constexpr (H < LR) {
+    f(std::integral_constant<int, H>{});
+    over_lanes<LR, 2 * H>(f);
+  }
+}
+
 // x[0..7] of the lanes of a row (D / 8 lanes, lane j holds channels 8 j ..):
 // unnormalized Sylvester butterflies over the row's channels.
 template <int D, typename T>
@@ -75,13 +99,21 @@ __device__ __forceinline__ void fwht_row(T (&x)[8], int j) {
         x[i] = a + b;
         x[i + s] = a - b;
       }
+  over_lanes<D / 8>([&](auto H) {
+    constexpr int h = decltype(H)::value;
+    const T sgn = (j & h) ? T(-1) : T(1);
 #pragma unroll
-  for (int s = 1; s < D / 8; s *= 2)
+    for (int i = 0; i < 8; ++i) x[i] = fma(sgn, x[i], lane_swap<h>(x[i]));
+  });
+}
+// Largest |x| of a row.
+template <int D, typename T>
+__device__ __forceinline__ T top_row(const T (&x)[8]) {
+  T top = 0;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      const T o = __shfl_xor(x[i], s);
-      x[i] = (j & s) ? o - x[i] : x[i] + o;
-    }
+  for (int i = 0; i < 8; ++i) top = fmax(top, fabs(x[i]));
+  over_lanes<D / 8>([&](auto H) { top = fmax(top, lane_swap<decltype(H)::value>(top)); });
+  return top;
 }
 
 // Code of one element: the integer nearest to 7 u / top, ties to even, |u| <=
@@ -90,118 +122,168 @@ __device__ __forceinline__ void fwht_row(T (&x)[8], int j) {
 // a half integer is decided exactly: the estimate is at most one off, and only
 // beside a boundary.
 template <typename T>
-__device__ __forceinline__ int code_of(T u, T top, T inv) {
-  T q = rint(u * inv);
+__device__ __forceinline__ float exact_code(T u, T top) {
+  const T q = rint(u * (T(7) / top));
   const T e = fma(-q, top, T(7) * u), d = T(2) * fabs(e) - top;
   const int n = static_cast<int>(q);
   const int up = e > T(0) ? 1 : -1;
-  return d > T(0) || (d == T(0) && (n & 1)) ? n + up : n;
+  return static_cast<float>(d > T(0) || (d == T(0) && (n & 1)) ? n + up : n);
+}
+// The codes of a lane's 8 channels as one word.  The fp32 quotient is within
+// 2^-19 of the exact one (7 times four roundings), so only a quotient within
+// 2^-16 of a half integer has to be decided exactly: ties mostly, which half the
+// waves of bf16 rows have, but in one or two of their 8 channels.
+template <typename T>
+__device__ __forceinline__ uint32_t codes8(const T (&u)[8], T top) {
+  const float inv = 7.0f * __builtin_amdgcn_rcpf(static_cast<float>(top));
+  const bool range = inv > 1e-30f && inv < 1e30f;
+  uint32_t w = 0;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    const float r = static_cast<float>(u[i]) * inv;
+    float q = rintf(r);
+    if (__builtin_amdgcn_ballot_w64(!(range && fabsf(r - q) < 0.5f - 0x1p-16f)) != 0) {
+      // (Scaled by a power of two to [1, 2), so that nothing overflows.)
+      const int e = top > 0 ? -ilogb(top) : 0;
+      q = top > 0 ? exact_code(ldexp(u[i], e), ldexp(top, e)) : 0;
+    }
+    w |= static_cast<uint32_t>(static_cast<int>(q) & 15) << (4 * i);
+  }
+  return w;
 }
 
 // ---------------------------------------------------------------------------
-// Append.  D / 8 lanes take one row of K or V.  HBM bound: 4 d bytes read and
-// d + 8 written per token and head.
+// Append.  HBM bound: 4 d bytes read and d + 8 written per token and head.
+//
+// A workgroup takes the keys and the values of 2048 / d tokens and one head, d / 8
+// lanes a row, both loads in flight from the start.  Rotated keys are summed in
+// fp64, where sums of inputs are exact; that is 8 us of the 30 that 16000 tokens
+// of 8 heads of 128 take (83 MB, 2.8 TB/s; unrotated 22 us, 3.8 TB/s), the rest of
+// it the vector work of max and codes beside the loads.  Codes of values go through LDS, so that a wave stores 16
+// tokens of a channel pair as neighbouring bytes: tokens of a prompt fill their
+// blocks with whole 16-byte runs whatever place they start at.
 // ---------------------------------------------------------------------------
+template <int D>
+struct Rows {
+  static constexpr int LR = D / 8, N = 256 / LR;  // lanes of a row, tokens of a workgroup
+};
+
+// blk / p16, and the remainder in `in`: inv = floor(2^32 / p16) (p16 = 1: 2^32 - 1)
+// gives the quotient or one less.
+__device__ __forceinline__ uint32_t div_blocks(uint32_t blk, uint32_t p16, uint32_t inv, uint32_t& in) {
+  uint32_t q = __umulhi(blk, inv);
+  in = blk - q * p16;
+  const bool over = in >= p16;
+  in -= over ? p16 : 0;
+  return q + (over ? 1 : 0);
+}
+// First token of the 16-token block that a slot's token lies in, in the
+// cache's order [page][head][token]; t: the token's place in the block.
+__device__ __forceinline__ int64_t slot_block(const Cache& c, int64_t slot, int h, int& t) {
+  uint32_t in;
+  const uint32_t page = div_blocks(static_cast<uint32_t>(slot >> 4), c.p16, c.p16_inv, in);
+  t = static_cast<int>(slot & 15);
+  return ((static_cast<int64_t>(page) * c.hk + h) * c.p16 + in) * 16;
+}
+
 template <int D, bool ROT, bool BF>
 __global__ __launch_bounds__(256) void kv4_append_kernel(Cache c, const uint16_t* K, const uint16_t* V, int64_t n,
                                                          int64_t ldk, int64_t ldv, const int64_t* slots) {
-  constexpr int LR = D / 8, RW = 256 / LR;
-  const int64_t row = static_cast<int64_t>(blockIdx.x) * RW + threadIdx.x / LR;
-  const int j = threadIdx.x % LR;
-  const bool is_v = blockIdx.y == 1;
-  const int64_t rr = row < n * c.hk ? row : 0;  // (lanes past the end keep the exchanges whole)
-  const int64_t tok = rr / c.hk;
-  const int h = static_cast<int>(rr % c.hk);
-  float x[8];
-  load8<BF>((is_v ? V + tok * ldv : K + tok * ldk) + h * D + 8 * j, x);
-  int q[8];
-  float scale;
-  if (ROT && !is_v) {
-    double u[8], top = 0;
+  constexpr int LR = Rows<D>::LR, N = Rows<D>::N;
+  __shared__ uint32_t sc[N][LR + 1];
+  const int h = blockIdx.x % c.hk;
+  const int64_t tok0 = static_cast<int64_t>(blockIdx.x / c.hk) * N;
+  const int r = threadIdx.x / LR, j = threadIdx.x % LR;  // row, 8 channels of it
+  const int vt = threadIdx.x % N, vj = threadIdx.x / N;  // the same for the stores of values
+  const int64_t tok = min(tok0 + r, n - 1), vtok = min(tok0 + vt, n - 1);
+  float v[8], k[8];
+  load8<BF>(V + tok * ldv + h * D + 8 * j, v);
+  load8<BF>(K + tok * ldk + h * D + 8 * j, k);
+  const int64_t slot = slots[tok], vslot = slots[vtok];
+  const bool ok = tok0 + r < n && slot >= 0 && slot < c.n_slots;
+  const bool vok = tok0 + vt < n && vslot >= 0 && vslot < c.n_slots;
+  const float vtop = top_row<D>(v);
+  sc[r][j] = codes8<float>(v, vtop);
+  uint32_t kw;
+  float ks;
+  if constexpr (ROT) {
+    double u[8];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) u[i] = x[i];
+    for (int i = 0; i < 8; ++i) u[i] = k[i];
     fwht_row<D>(u, j);
-#pragma unroll
-    for (int i = 0; i < 8; ++i) top = fmax(top, fabs(u[i]));
-#pragma unroll
-    for (int s = 1; s < LR; s *= 2) top = fmax(top, __shfl_xor(top, s));
-    const double inv = 7.0 / top;
-#pragma unroll
-    for (int i = 0; i < 8; ++i) q[i] = top > 0 ? code_of<double>(u[i], top, inv) : 0;
-    scale = static_cast<float>(top / (7.0 * sqrt(static_cast<double>(D))));
+    const double top = top_row<D>(u);
+    kw = codes8<double>(u, top);
+    ks = static_cast<float>(top * (1.0 / (7.0 * __builtin_sqrt(static_cast<double>(D)))));
   } else {
-    float top = 0;
-#pragma unroll
-    for (int i = 0; i < 8; ++i) top = fmaxf(top, fabsf(x[i]));
-#pragma unroll
-    for (int s = 1; s < LR; s *= 2) top = fmaxf(top, __shfl_xor(top, s));
-    // (Scaled by a power of two to [1, 2), so that nothing overflows.)
-    const int e = top > 0 ? -ilogbf(top) : 0;
-    const float t = ldexpf(top, e), inv = 7.0f / t;
-#pragma unroll
-    for (int i = 0; i < 8; ++i) q[i] = top > 0 ? code_of<float>(ldexpf(x[i], e), t, inv) : 0;
-    scale = top / 7.0f;
+    const float top = top_row<D>(k);
+    kw = codes8<float>(k, top);
+    ks = top / 7.0f;
   }
-  const int64_t slot = row < n * c.hk ? slots[tok] : -1;
-  if (slot < 0 || slot >= c.n_slots) return;
-  const int64_t page = slot / c.page;
-  const int t = static_cast<int>(slot % c.page);
-  const int64_t base = (page * c.hk + h) * c.page;  // rows of D / 2 bytes before this page's head
-  uint32_t b[4];
-#pragma unroll
-  for (int i = 0; i < 4; ++i) b[i] = (q[2 * i] & 15) | (q[2 * i + 1] & 15) << 4;
-  if (!is_v) {
-    *reinterpret_cast<uint32_t*>(c.kc + (base + t) * (D / 2) + 4 * j) = b[0] | b[1] << 8 | b[2] << 16 | b[3] << 24;
-    if (j == 0) c.ks[base + t] = scale;
-  } else {
-    uint8_t* o = c.vc + (base + (t & ~15)) * (D / 2) + (t & 15) + 64 * j;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) o[16 * i] = static_cast<uint8_t>(b[i]);
-    if (j == 0) c.vs[base + t] = scale;
+  if (ok) {
+    int t;
+    const int64_t row = slot_block(c, slot, h, t) + t;
+    *reinterpret_cast<uint32_t*>(c.kc + row * (D / 2) + 4 * j) = kw;
+    if (j == 0) {
+      c.ks[row] = ks;
+      c.vs[row] = vtop / 7.0f;
+    }
   }
+  __syncthreads();
+  if (!vok) return;
+  int t;
+  uint8_t* o = c.vc + slot_block(c, vslot, h, t) * (D / 2) + 64 * vj;
+  const uint32_t w = sc[vt][vj];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) o[16 * i + t] = static_cast<uint8_t>(w >> (8 * i));
 }
 
 // ---------------------------------------------------------------------------
 // Gather: the values of cached rows (slots out of range give zeros), keys
-// rotated back.
+// rotated back.  Workgroups as in append, the bytes of values read with a
+// token a lane and turned in LDS.
 // ---------------------------------------------------------------------------
 template <int D, bool ROT>
 __global__ __launch_bounds__(256) void kv4_gather_kernel(Cache c, const int64_t* slots, int64_t n, void* K, void* V,
                                                          int64_t ldk, int64_t ldv, int dtype) {
-  constexpr int LR = D / 8, RW = 256 / LR;
-  const int64_t row = static_cast<int64_t>(blockIdx.x) * RW + threadIdx.x / LR;
-  const int j = threadIdx.x % LR;
+  constexpr int LR = Rows<D>::LR, N = Rows<D>::N;
+  __shared__ uint32_t sc[N][LR + 1];
+  const int h = blockIdx.x % c.hk;
+  const int64_t tok0 = static_cast<int64_t>(blockIdx.x / c.hk) * N;
+  const int r = threadIdx.x / LR, j = threadIdx.x % LR;
   const bool is_v = blockIdx.y == 1;
-  const bool in = row < n * c.hk;
-  const int64_t tok = in ? row / c.hk : 0;
-  const int h = in ? static_cast<int>(row % c.hk) : 0;
-  int64_t slot = slots[tok];
-  const bool ok = slot >= 0 && slot < c.n_slots;
-  slot = ok ? slot : 0;
-  const int64_t page = slot / c.page;
-  const int t = static_cast<int>(slot % c.page);
-  const int64_t base = (page * c.hk + h) * c.page;
-  uint32_t w;
+  auto find = [&](int64_t i, int& t) -> int64_t {  // the block of token i's slot, -1: none
+    const int64_t slot = i < n ? slots[i] : -1;
+    return slot >= 0 && slot < c.n_slots ? slot_block(c, slot, h, t) : -1;
+  };
+  int t = 0;
+  const int64_t base = find(tok0 + r, t);
+  float scale = base >= 0 ? (is_v ? c.vs : c.ks)[base + t] : 0.0f;
+  uint32_t w = 0;
   if (!is_v) {
-    w = *reinterpret_cast<const uint32_t*>(c.kc + (base + t) * (D / 2) + 4 * j);
+    if (base >= 0) w = *reinterpret_cast<const uint32_t*>(c.kc + (base + t) * (D / 2) + 4 * j);
   } else {
-    const uint8_t* p = c.vc + (base + (t & ~15)) * (D / 2) + (t & 15) + 64 * j;
-    w = p[0] | p[16] << 8 | p[32] << 16 | static_cast<uint32_t>(p[48]) << 24;
+    const int vt = threadIdx.x % N, vj = threadIdx.x / N;
+    int tt = 0;
+    const int64_t vb = find(tok0 + vt, tt);
+    if (vb >= 0) {
+      const uint8_t* p = c.vc + vb * (D / 2) + tt + 64 * vj;
+      w = p[0] | p[16] << 8 | p[32] << 16 | static_cast<uint32_t>(p[48]) << 24;
+    }
+    sc[vt][vj] = w;
+    __syncthreads();
+    w = sc[r][j];
   }
-  float scale = (is_v ? c.vs : c.ks)[base + t];
-  scale = ok ? scale : 0.0f;
-  w = ok ? w : 0;
   float x[8];
 #pragma unroll
   for (int i = 0; i < 8; ++i) x[i] = static_cast<float>(static_cast<int32_t>(w << (28 - 4 * i)) >> 28);
   if (ROT && !is_v) {
     fwht_row<D>(x, j);  // sums of up to 256 codes, exact
-    scale *= 1.0f / sqrtf(static_cast<float>(D));
+    scale *= 1.0f / __builtin_sqrtf(static_cast<float>(D));
   }
 #pragma unroll
   for (int i = 0; i < 8; ++i) x[i] *= scale;
-  if (!in) return;
-  const int64_t off = tok * (is_v ? ldv : ldk) + h * D + 8 * j;
+  if (tok0 + r >= n) return;
+  const int64_t off = (tok0 + r) * (is_v ? ldv : ldk) + h * D + 8 * j;
   if (dtype == OQ_OUT_F32) {
     float4* o = reinterpret_cast<float4*>(static_cast<float*>(is_v ? V : K) + off);
     o[0] = make_float4(x[0], x[1], x[2], x[3]);
@@ -256,8 +338,6 @@ struct AttnKv4 {
   uint32_t n_pages, page_blocks;  // page_blocks: 16-token blocks of a page, all heads
   int table_last;                 // last index of a table row
   int n_seqs, hq, R, max_q, max_len, splits, chunk;  // chunk: tokens of a split, a multiple of kTile
-  int p16;         // 16-token blocks of a page
-  uint32_t p16_inv;  // floor(2^32 / p16) (p16 = 1: 2^32 - 1)
   float scale_log2e;
   bool causal;
 };
@@ -351,15 +431,12 @@ __global__ __launch_bounds__(64 * W, QT == 1 ? D < 256 ? 3 : 2 : 1) void attn_kv
   const int c0 = split * a.chunk, first = c0 + wave * kTile;  // tokens
   const int32_t* table = a.table + b * a.table_ld;
   // Page table entry of 16-token block `blk` of the sequence, and the block's place in the page.
-  auto entry = [&](int blk, int& in) -> int {
-    int pi = static_cast<int>(__umulhi(static_cast<uint32_t>(blk), a.p16_inv));
-    in = blk - pi * a.p16;
-    const bool over = in >= a.p16;
-    pi += over ? 1 : 0;
-    in -= over ? a.p16 : 0;
+  auto entry = [&](int blk, uint32_t& in) -> int {
+    const int pi = static_cast<int>(div_blocks(static_cast<uint32_t>(blk), a.c.p16, a.c.p16_inv, in));
     return table[min(pi, a.table_last)];  // (tokens past the row's width are past max_len: not used)
   };
-  int in_page, page = entry(first / 16 + g, in_page);
+  uint32_t in_page;
+  int page = entry(first / 16 + g, in_page);
   const int L = __builtin_amdgcn_readfirstlane(max(0, min(a.lens[b], a.max_len)));
   int q0, nq;
   query_rows(a, b, q0, nq);
@@ -372,9 +449,9 @@ __global__ __launch_bounds__(64 * W, QT == 1 ? D < 256 ? 3 : 2 : 1) void attn_kv
   // A 16-token block of the cache that this lane group's tokens lie in (0 where they have none).
   bool own_ok;
   uint32_t own;
-  auto place = [&](int pg, int in, int tok) {
+  auto place = [&](int pg, uint32_t in, int tok) {
     own_ok = tok < L && static_cast<uint32_t>(pg) < a.n_pages;
-    own = static_cast<uint32_t>(own_ok ? pg : 0) * a.page_blocks + h * a.p16 + (own_ok ? in : 0);
+    own = static_cast<uint32_t>(own_ok ? pg : 0) * a.page_blocks + h * a.c.p16 + (own_ok ? in : 0);
   };
   uint4 kr[4][D >= 128 ? KW / 4 : 1];
   auto load_keys = [&]() {
@@ -786,7 +863,9 @@ int cache_validate(const oq_kv4_cache* c) {
 }
 
 Cache device_cache(const oq_kv4_cache* c) {
-  return Cache{c->k_codes, c->v_codes, c->k_scale, c->v_scale, c->n_pages * c->page_tokens, c->page_tokens, c->n_kv_heads};
+  const uint32_t p16 = static_cast<uint32_t>(c->page_tokens / 16);
+  return Cache{c->k_codes, c->v_codes, c->k_scale, c->v_scale, c->n_pages * c->page_tokens, c->n_kv_heads, p16,
+               p16 == 1 ? UINT32_MAX : static_cast<uint32_t>((uint64_t{1} << 32) / p16)};
 }
 
 // The launch.  Rows: 16 columns of products (two such blocks in a workgroup above
@@ -865,9 +944,9 @@ extern "C" int oq_kv4_append(const oq_kv4_cache* cache, const void* K, const voi
   if (!oq::aligned(K, 16) || !oq::aligned(V, 16) || !oq::aligned(slots, 8)) return OQ_ERR_ALIGN;
   if ((st = oq::device_check()) != OQ_OK) return st;
   const oq::Cache c = oq::device_cache(cache);
-  const int64_t per = 2048 / cache->head_dim, blocks = (n * c.hk + per - 1) / per;
+  const int64_t per = 2048 / cache->head_dim, blocks = (n + per - 1) / per * c.hk;
   if (blocks > INT32_MAX) return OQ_ERR_SHAPE;
-  const dim3 grid(static_cast<unsigned>(blocks), 2);
+  const dim3 grid(static_cast<unsigned>(blocks));
   const bool bf = dtype == OQ_OUT_BF16;
   hipStream_t s = static_cast<hipStream_t>(stream);
 #define OQ_APPEND(D, R, B)                                                                                            \
@@ -900,7 +979,7 @@ extern "C" int oq_kv4_gather(const oq_kv4_cache* cache, const int64_t* slots, in
   if (!oq::aligned(K, 16) || !oq::aligned(V, 16) || !oq::aligned(slots, 8)) return OQ_ERR_ALIGN;
   if ((st = oq::device_check()) != OQ_OK) return st;
   const oq::Cache c = oq::device_cache(cache);
-  const int64_t per = 2048 / cache->head_dim, blocks = (n * c.hk + per - 1) / per;
+  const int64_t per = 2048 / cache->head_dim, blocks = (n + per - 1) / per * c.hk;
   if (blocks > INT32_MAX) return OQ_ERR_SHAPE;
   const dim3 grid(static_cast<unsigned>(blocks), 2);
   hipStream_t s = static_cast<hipStream_t>(stream);
@@ -983,8 +1062,6 @@ extern "C" int oq_attention_kv4(const oq_kv4_cache* cache, const void* Q, int64_
   a.max_len = max_len;
   a.splits = p.splits;
   a.chunk = p.chunk;
-  a.p16 = cache->page_tokens / 16;
-  a.p16_inv = a.p16 == 1 ? 0xFFFFFFFFu : static_cast<uint32_t>((uint64_t{1} << 32) / a.p16);
   a.scale_log2e = scale * 1.4426950408889634f;
   a.causal = causal == 1;
   const dim3 grid(static_cast<unsigned>(p.row_blocks), static_cast<unsigned>(n_seqs * cache->n_kv_heads),
