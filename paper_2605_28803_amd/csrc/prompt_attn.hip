@@ -1,7 +1,7 @@
 // Softmax self-attention within packed sequences (prompts), grouped heads,
 // causal or full.
 //
-// A workgroup of 4 waves takes 128 QT query tokens of one sequence and head
+// A workgroup takes 32 query tokens a row wave (4, 128 tokens) of one sequence and head
 // and walks the sequence's keys in steps of BN with a running maximum m and sum l
 // per row (one pass over K and V; nothing of the pair matrix leaves the
 // registers).  Both products are transposed, on v_mfma_f32_32x32x16: S^T = K Q^T
@@ -12,6 +12,14 @@
 // read, four keys of a channel a lane.  K and V tiles go from global memory into
 // two LDS buffers with 16-byte direct loads, the next tile's while this one is
 // multiplied, one barrier per step.
+//
+// What bounds it: at d = 128 a step of 64 keys and 32 rows costs a wave 1024
+// cycles of matrix instructions, about 700 of the vector unit (32 exponentials at a
+// quarter of its rate, as many multiply-adds, half as many maxima, packed roundings and dot
+// products that add the rounded probabilities) and 32 KB of LDS reads; two waves a SIMD
+// overlap them.  One causal sequence of 8192, 32 / 8 heads of 128: 561 us, 980
+// TFLOP/s, 83% of what the library's 8192-cubed bf16 product reaches on the same card; 64 rows
+// a wave (half the LDS reads, one wave a SIMD) 857 us; 32-key steps 604.
 //
 // LDS rows are not padded; 16-byte pieces of a row are stored at piece ^ a
 // function of the row.  K: 16 rows of one piece cover all banks.  V: 4 rows of 4
@@ -79,25 +87,36 @@ struct Half<true> {
   }
 };
 
-template <bool BF, int D, int QT, int BN>
-__global__ __launch_bounds__(256, QT == 1 ? 2 : 1) void prompt_attn_kernel(PromptArgs a) {
+template <bool BF, int D, int BN, int RW, int KG>
+__global__ __launch_bounds__(64 * RW * KG, 2) void prompt_attn_kernel(PromptArgs a) {
   typedef Half<BF> H;
   typedef typename H::v8 v8;
-  constexpr int BM = 128 * QT, PCS = D / 8, ROWB = 2 * D;
+  constexpr int BM = 32 * RW, PCS = D / 8, ROWB = 2 * D;
   constexpr int KB = BN * ROWB, STAGE = 2 * KB;
-  constexpr int LK = KB / 1024 / 4;  // 1 KB loads of K (and of V) per wave and tile
+  constexpr int LK = KB / 1024 / RW;  // 1 KB loads of K (and of V) per wave and tile
   constexpr int SUB = BN / 32, CT = D / 32, KS = D / 16;
-  __shared__ __attribute__((aligned(16))) uint8_t smem[2 * STAGE];
+  constexpr int JOINB = KG > 1 ? (KG - 1) * RW * 64 * (16 * CT + 2) * 4 : 0;
+  __shared__ __attribute__((aligned(16))) uint8_t smem[2 * STAGE * KG > JOINB ? 2 * STAGE * KG : JOINB];
 
-  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int lane = threadIdx.x & 63, wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int wave = wv % RW, grp = wv / RW;
   const int col = lane & 31, h = lane >> 5;
-  // Consecutive ids go to different XCDs (id % 8): XCD x takes the x-th
-  // contiguous part of (head, tile), so that heads which share K and V share its L2.
-  const int total = a.hq * a.tiles;
-  const int id = blockIdx.x, per = total >> 3, rem = total & 7, x = id & 7;
-  const int lin = x * per + min(x, rem) + (id >> 3);
-  const int head = lin / a.tiles;
-  int tile = lin % a.tiles;
+  // Consecutive ids go to different XCDs (id % 8).  With a multiple of 8 heads an
+  // XCD takes whole heads, so that those which share K and V share its L2; else
+  // the heads go round.  Tiles come in falling order (the later a causal tile, the
+  // more keys it has), but where a CU holds several workgroups the second of each
+  // of an XCD's 32 CUs in rising order, so that long and short ones meet (one
+  // causal sequence of 4096, 32 / 8 heads of 128: 180 -> 151 us).
+  const int id = blockIdx.x;
+  int head, tile;
+  {
+    const bool whole = a.hq % 8 == 0;
+    const int heads = whole ? a.hq / 8 : a.hq, cus = whole ? 32 : 256, n = heads * a.tiles;
+    int k = whole ? id >> 3 : id;
+    if ((KG == 1 || D == 64) && k >= cus && k < 2 * cus) k = min(2 * cus, n) - 1 - (k - cus);
+    tile = k / heads;
+    head = (whole ? (id & 7) * heads : 0) + k % heads;
+  }
   // The tile's sequence: a running count of the sequences' tiles, 64 at a time.
   int lo = 0, hi = 0, found = 0;
   for (int s0 = 0; s0 < a.n_seqs; s0 += 64) {
@@ -129,11 +148,12 @@ __global__ __launch_bounds__(256, QT == 1 ? 2 : 1) void prompt_attn_kernel(Promp
   if (!found) return;
   const int r0 = lo + tile * BM;
   const int kend = a.causal ? min(hi, r0 + BM) : hi;
-  const int wrow = r0 + wave * 32 * QT;  // the wave's first row
+  const int wrow = r0 + wave * 32;  // the wave's first row
 
   const uint16_t* kbase = a.k + (head / a.rep) * D + static_cast<int64_t>(lo) * a.ldk;
   const uint16_t* vbase = a.v + (head / a.rep) * D + static_cast<int64_t>(lo) * a.ldv;
-  const uint32_t lds0 = static_cast<uint32_t>(reinterpret_cast<uintptr_t>((__attribute__((address_space(3))) uint8_t*)smem));
+  const uint32_t ring = grp * 2 * STAGE;  // the key group's two buffers
+  const uint32_t lds0 = ring + static_cast<uint32_t>(reinterpret_cast<uintptr_t>((__attribute__((address_space(3))) uint8_t*)smem));
   const uint32_t ldk2 = static_cast<uint32_t>(2 * a.ldk), ldv2 = static_cast<uint32_t>(2 * a.ldv);
   auto swzk = [](int row) { return PCS == 8 ? (row >> 1) & 7 : row & 15; };
   auto swzv = [](int row) { return PCS == 8 ? ((row >> 1) & 1) << 2 : (row & 3) << 2; };
@@ -150,104 +170,103 @@ __global__ __launch_bounds__(256, QT == 1 ? 2 : 1) void prompt_attn_kernel(Promp
       dma16(lds0 + buf * STAGE + KB + l * 1024, rr * ldv2 + 16 * (slot ^ swzv(row)), vb);
     }
   };
-  issue(lo, 0);
+  const int k_first = lo + grp * BN;
+  if (k_first < kend) issue(k_first, 0);
 
-  v8 qf[QT][KS];
-#pragma unroll
-  for (int t = 0; t < QT; ++t) {
-    const int r = min(wrow + 32 * t + col, hi - 1);
+  v8 qf[KS];
+  {
+    const int r = min(wrow + col, hi - 1);
     const uint16_t* qp = a.q + static_cast<int64_t>(r) * a.ldq + head * D + 8 * h;
 #pragma unroll
-    for (int ks = 0; ks < KS; ++ks) qf[t][ks] = *reinterpret_cast<const v8*>(qp + 16 * ks);
+    for (int ks = 0; ks < KS; ++ks) qf[ks] = *reinterpret_cast<const v8*>(qp + 16 * ks);
   }
-  v16f acc[QT][CT];
-  float m[QT], l[QT];
+  v16f acc[CT];
+  float m = -INFINITY, l = 0.0f;
 #pragma unroll
-  for (int t = 0; t < QT; ++t) {
-    m[t] = -INFINITY;
-    l[t] = 0.0f;
+  for (int c = 0; c < CT; ++c)
 #pragma unroll
-    for (int c = 0; c < CT; ++c)
+    for (int e = 0; e < 16; ++e) acc[c][e] = 0.0f;
+  // LDS byte offsets of this lane's reads within a buffer; the rest of an address is constant.
+  // K: row 32 u + col, piece 2 ks + h at slot piece ^ swzk(col): 2 ks differs from
+  // (2 ks) % (2 KO) by whole runs of 2 KO pieces, which the exclusive or leaves.
+  constexpr int KO = KS < 8 ? KS : 8;
+  uint32_t koff[KO];
 #pragma unroll
-      for (int e = 0; e < 16; ++e) acc[t][c][e] = 0.0f;
-  }
-  // Addresses of this lane's reads.
-  const int vi = lane & 15, vg = (lane >> 4) & 1;
+  for (int i = 0; i < KO; ++i) koff[i] = ring + col * ROWB + (((2 * i) ^ h ^ swzk(col)) << 4);
+  // V: row 32 u + 16 j + 8 y + 4 h + vi / 4, channels 32 ct + 16 vg + 4 (vi % 4).
+  constexpr int VO = CT < 4 ? CT : 4;
+  const int vi = lane & 15, vg = (lane >> 4) & 1, vrow = 4 * h + (vi >> 2);
+  uint32_t voff[VO];
+#pragma unroll
+  for (int i = 0; i < VO; ++i)
+    voff[i] = ring + KB + vrow * ROWB + (((4 * i + 2 * vg + ((vi & 3) >> 1)) ^ swzv(vrow)) << 4) + 8 * (vi & 1);
   const float c = a.scale_log2e;
-  int buf = 0;
-  for (int k0 = lo; k0 < kend; k0 += BN, buf ^= 1) {
+  uint32_t buf = 0;
+  // (Every wave passes every barrier: the groups take the same number of steps.)
+  for (int k0 = k_first, kb0 = lo; kb0 < kend; k0 += KG * BN, kb0 += KG * BN, buf ^= 1) {
     asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
     __builtin_amdgcn_s_barrier();
     asm volatile("" ::: "memory");
-    if (k0 + BN < kend) issue(k0 + BN, buf ^ 1);
-    const int wlast = min(wrow + 32 * QT, hi) - 1;
-    if (a.causal && k0 > wlast) continue;  // (this wave's rows see none of the tile)
-    const uint8_t* sk = smem + buf * STAGE;
-    const uint8_t* sv = sk + KB;
-    v16f s[QT][SUB];
-#pragma unroll
-    for (int t = 0; t < QT; ++t)
-#pragma unroll
-      for (int u = 0; u < SUB; ++u)
-#pragma unroll
-        for (int e = 0; e < 16; ++e) s[t][u][e] = 0.0f;
+    if (k0 + KG * BN < kend) issue(k0 + KG * BN, buf ^ 1);
+    const int wlast = min(wrow + 32, hi) - 1;
+    if (k0 >= kend || (a.causal && k0 > wlast)) continue;  // (this wave's rows see none of the tile)
+    const uint8_t* sb = smem + buf * STAGE;
+    v16f s[SUB];
 #pragma unroll
     for (int u = 0; u < SUB; ++u)
 #pragma unroll
-      for (int ks = 0; ks < KS; ++ks) {
-        const int row = 32 * u + col;
-        const v8 kf = *reinterpret_cast<const v8*>(sk + row * ROWB + (((2 * ks + h) ^ swzk(row)) * 16));
+      for (int e = 0; e < 16; ++e) s[u][e] = 0.0f;
 #pragma unroll
-        for (int t = 0; t < QT; ++t) s[t][u] = H::mfma(kf, qf[t][ks], s[t][u]);
+    for (int ks = 0; ks < KS; ++ks)
+#pragma unroll
+      for (int u = 0; u < SUB; ++u) {
+        const v8 kf = *reinterpret_cast<const v8*>(sb + koff[ks % KO] + (ks / KO) * (32 * KO) + 32 * u * ROWB);
+        s[u] = H::mfma(kf, qf[ks], s[u]);
       }
     // Masked tiles: past the end, or on the diagonal.
     if (k0 + BN > hi || (a.causal && k0 + BN - 1 > wrow)) {
+      const int r = min(wrow + col, hi - 1);
+      const int left = (a.causal ? r + 1 : hi) - k0 - 4 * h;
 #pragma unroll
-      for (int t = 0; t < QT; ++t) {
-        const int r = min(wrow + 32 * t + col, hi - 1);
-        const int end = a.causal ? r + 1 : hi;
+      for (int u = 0; u < SUB; ++u)
 #pragma unroll
-        for (int u = 0; u < SUB; ++u)
-#pragma unroll
-          for (int e = 0; e < 16; ++e)
-            if (k0 + 32 * u + 8 * (e / 4) + 4 * h + e % 4 >= end) s[t][u][e] = -INFINITY;
-      }
+        for (int e = 0; e < 16; ++e)
+          if (32 * u + 8 * (e / 4) + e % 4 >= left) s[u][e] = -INFINITY;
     }
-    v8 pf[QT][SUB][2];
+    float top = s[0][0];
 #pragma unroll
-    for (int t = 0; t < QT; ++t) {
-      float top = s[t][0][0];
+    for (int u = 0; u < SUB; ++u)
 #pragma unroll
-      for (int u = 0; u < SUB; ++u)
+      for (int e = 0; e < 16; ++e) top = fmaxf(top, s[u][e]);
+    top = fmaxf(top, rqd::lane_xor_far<32>(top));
+    const float mn = fmaxf(m, top * c);
+    if (__builtin_amdgcn_ballot_w64(mn > m) != 0) {
+      // (With key groups a row may have seen nothing yet.)
+      const float al = KG > 1 && mn == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(m - mn);
+      l *= al;
 #pragma unroll
-        for (int e = 0; e < 16; ++e) top = fmaxf(top, s[t][u][e]);
-      top = fmaxf(top, rqd::lane_xor_far<32>(top));
-      const float mn = fmaxf(m[t], top * c);
-      if (__builtin_amdgcn_ballot_w64(mn > m[t]) != 0) {
-        const float al = __builtin_amdgcn_exp2f(m[t] - mn);
-        l[t] *= al;
+      for (int ct = 0; ct < CT; ++ct)
 #pragma unroll
-        for (int ct = 0; ct < CT; ++ct)
+        for (int e = 0; e < 16; ++e) acc[ct][e] *= al;
+      m = mn;
+    }
+    const float mr = KG > 1 && mn == -INFINITY ? 0.0f : mn;
+    v8 pf[SUB][2];
 #pragma unroll
-          for (int e = 0; e < 16; ++e) acc[t][ct][e] *= al;
-        m[t] = mn;
-      }
+    for (int u = 0; u < SUB; ++u)
 #pragma unroll
-      for (int u = 0; u < SUB; ++u)
+      for (int j = 0; j < 2; ++j) {
+        uint4 pk;
+        uint32_t* w = &pk.x;
 #pragma unroll
-        for (int j = 0; j < 2; ++j) {
-          uint4 pk;
-          uint32_t* w = &pk.x;
-#pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            const float p0 = __builtin_amdgcn_exp2f(fmaf(s[t][u][8 * j + 2 * i], c, -mn));
-            const float p1 = __builtin_amdgcn_exp2f(fmaf(s[t][u][8 * j + 2 * i + 1], c, -mn));
-            w[i] = H::pack(p0, p1);
-            l[t] = H::add2(w[i], l[t]);
-          }
-          pf[t][u][j] = __builtin_bit_cast(v8, pk);
+        for (int i = 0; i < 4; ++i) {
+          const float p0 = __builtin_amdgcn_exp2f(fmaf(s[u][8 * j + 2 * i], c, -mr));
+          const float p1 = __builtin_amdgcn_exp2f(fmaf(s[u][8 * j + 2 * i + 1], c, -mr));
+          w[i] = H::pack(p0, p1);
+          l = H::add2(w[i], l);
         }
-    }
+        pf[u][j] = __builtin_bit_cast(v8, pk);
+      }
 #pragma unroll
     for (int ct = 0; ct < CT; ++ct)
 #pragma unroll
@@ -259,43 +278,90 @@ __global__ __launch_bounds__(256, QT == 1 ? 2 : 1) void prompt_attn_kernel(Promp
             v8 o;
           } vf;
 #pragma unroll
-          for (int y = 0; y < 2; ++y) {
-            const int row = 32 * u + 16 * j + 8 * y + 4 * h + (vi >> 2);
-            const int piece = 4 * ct + 2 * vg + ((vi & 3) >> 1);
-            const uint8_t* p = sv + row * ROWB + (piece ^ swzv(row)) * 16 + 8 * (vi & 1);
+          for (int y = 0; y < 2; ++y)
             vf.q[y] = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
-                (__attribute__((address_space(3))) v4s*)(reinterpret_cast<v4s*>(const_cast<uint8_t*>(p))));
-          }
-#pragma unroll
-          for (int t = 0; t < QT; ++t) acc[t][ct] = H::mfma(vf.o, pf[t][u][j], acc[t][ct]);
+                (__attribute__((address_space(3))) v4s*)(reinterpret_cast<v4s*>(const_cast<uint8_t*>(
+                    sb + voff[ct % VO] + (ct / VO) * (64 * VO) + (32 * u + 16 * j + 8 * y) * ROWB))));
+          acc[ct] = H::mfma(vf.o, pf[u][j], acc[ct]);
         }
   }
+  l += rqd::lane_xor_far<32>(l);
+  if constexpr (KG > 1) {
+    // The groups' outputs, through LDS in the accumulators' own order.
+    __syncthreads();
+    float* part = reinterpret_cast<float*>(smem);
+    constexpr int REGS = 16 * CT + 2;
+    if (grp > 0) {
+      float* o = part + ((grp - 1) * RW + wave) * 64 * REGS + lane;
 #pragma unroll
-  for (int t = 0; t < QT; ++t) {
-    const int r = wrow + 32 * t + col;
-    const float sum = l[t] + rqd::lane_xor_far<32>(l[t]);
-    const float inv = 1.0f / sum;
-    if (r >= hi) continue;
-    uint16_t* op = a.o + static_cast<int64_t>(r) * a.ldo + head * D + 4 * h;
+      for (int ct = 0; ct < CT; ++ct)
 #pragma unroll
-    for (int ct = 0; ct < CT; ++ct)
+        for (int e = 0; e < 16; ++e) o[64 * (16 * ct + e)] = acc[ct][e];
+      o[64 * 16 * CT] = m;
+      o[64 * (16 * CT + 1)] = l;
+    }
+    __syncthreads();
+    if (grp > 0) return;
 #pragma unroll
-      for (int q = 0; q < 4; ++q)
-        *reinterpret_cast<uint2*>(op + 32 * ct + 8 * q) =
-            make_uint2(H::pack(acc[t][ct][4 * q] * inv, acc[t][ct][4 * q + 1] * inv),
-                       H::pack(acc[t][ct][4 * q + 2] * inv, acc[t][ct][4 * q + 3] * inv));
+    for (int g = 1; g < KG; ++g) {
+      const float* o = part + ((g - 1) * RW + wave) * 64 * REGS + lane;
+      const float m2 = o[64 * 16 * CT], l2 = o[64 * (16 * CT + 1)];
+      const float mn = fmaxf(m, m2);  // (group 0 has the sequence's first key, which every row of a full or causal mask sees)
+      const float f1 = __builtin_amdgcn_exp2f(m - mn), f2 = __builtin_amdgcn_exp2f(m2 - mn);
+      m = mn;
+      l = l * f1 + l2 * f2;
+#pragma unroll
+      for (int ct = 0; ct < CT; ++ct)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) acc[ct][e] = acc[ct][e] * f1 + o[64 * (16 * ct + e)] * f2;
+    }
   }
+  const int r = wrow + col;
+  if (r >= hi) return;
+  const float inv = 1.0f / l;
+  uint16_t* op = a.o + static_cast<int64_t>(r) * a.ldo + head * D + 4 * h;
+#pragma unroll
+  for (int ct = 0; ct < CT; ++ct)
+#pragma unroll
+    for (int q = 0; q < 4; ++q)
+      *reinterpret_cast<uint2*>(op + 32 * ct + 8 * q) = make_uint2(H::pack(acc[ct][4 * q] * inv, acc[ct][4 * q + 1] * inv),
+                                                                   H::pack(acc[ct][4 * q + 2] * inv, acc[ct][4 * q + 3] * inv));
 }
 
-template <bool BF, int D, int QT, int BN>
+template <bool BF, int D, int BN, int RW, int KG>
 int launch_prompt(PromptArgs a, hipStream_t st) {
-  constexpr int BM = 128 * QT;
+  constexpr int BM = 32 * RW;
   const int64_t tiles = (static_cast<int64_t>(a.tokens) + BM - 1) / BM + a.n_seqs;
   const int64_t total = tiles * a.hq;
   if (total > INT32_MAX) return OQ_ERR_SHAPE;
   a.tiles = static_cast<int>(tiles);
-  hipLaunchKernelGGL((prompt_attn_kernel<BF, D, QT, BN>), dim3(static_cast<unsigned>(total)), dim3(256), 0, st, a);
+  hipLaunchKernelGGL((prompt_attn_kernel<BF, D, BN, RW, KG>), dim3(static_cast<unsigned>(total)), dim3(64 * RW * KG), 0, st, a);
   return launch_status();
+}
+// Shape of a workgroup: row waves of 32 queries, key groups.  Key groups take the
+// key tiles in turn and are joined at the end; they pay where there are fewer
+// workgroups than the card holds (two a CU for d >= 128) and sequences are long
+// enough for each to have several steps, since a row's walk over its keys
+// is then what takes the time.  wgs: workgroups of 128 rows, len: mean length.  Us with one
+// group against two (d = 64: four waves of rows):
+//   d = 128, causal: 1 x 816, 8 heads (wgs 56) 21.8 / 18.7; 1 x 2048, 16 heads (272) 54 / 42; 1 x 4096, 16
+//     (528) 103 / 88; 1 x 8192, 8 (520) 194 / 159; but 1 x 2500, 32 (656) 72 / 83; 4 x 1024, 16 (576) 33 / 48; 2 x 130, 16 (48)
+//     7.7 / 9.2; full: 4 x 700, 8 (200) 23 / 20; 1 x 4096, 16 (528) 145 / 157;
+//   d = 256, causal: 1 x 816, 8 45 / 37; 1 x 4096, 16 (528) 211 / 174; 4 x 1024, 16 (576) 66 / 91; full: 5 x 816, 8 (280) 52 / 42;
+//     1 x 3750, 16 (480) 245 / 271;
+//   d = 64 (a CU holds four, or two of two groups): 1 x 4096, 16 75 / 56; 1 x 2500, 32 50 / 42; 4 x 300, 16 (208) 8.2 / 8.0;
+//     48 ragged up to 600, 16 (1616) 23.6 / 27.0; four groups of 64 rows: 1 x 816, 8 (56) 15.4 / 12.7 / 10.2, but
+//     4 x 700, 8 (200) 16.0 / 13.3 / 19.2.
+template <bool BF>
+int launch_prompt_any(const PromptArgs& a, int d, hipStream_t st) {
+  const int64_t wgs = (static_cast<int64_t>(a.tokens) / 128 + a.n_seqs) * a.hq, len = a.tokens / a.n_seqs;
+  if (d == 64) {
+    if (wgs <= 144 && len >= 384) return launch_prompt<BF, 64, 64, 2, 4>(a, st);
+    return len >= 256 ? launch_prompt<BF, 64, 64, 4, 2>(a, st) : launch_prompt<BF, 64, 64, 4, 1>(a, st);
+  }
+  const bool two = (wgs <= 300 && len >= 256) || (a.causal && wgs <= 544 && len >= 2048);
+  if (d == 128) return two ? launch_prompt<BF, 128, 64, 4, 2>(a, st) : launch_prompt<BF, 128, 64, 4, 1>(a, st);
+  return two ? launch_prompt<BF, 256, 32, 4, 2>(a, st) : launch_prompt<BF, 256, 32, 4, 1>(a, st);
 }
 
 }  // namespace
@@ -326,10 +392,5 @@ extern "C" int oq_attention_prompt(const void* Q, const void* K, const void* V, 
                    static_cast<uint16_t*>(O), cu_seqlens, ldq, ldk, ldv, ldo, static_cast<int>(tokens), n_seqs, n_heads,
                    n_heads / n_kv_heads, 0, scale * 1.4426950408889634f, causal == 1};
   hipStream_t s = static_cast<hipStream_t>(stream);
-  const bool bf = dtype == OQ_OUT_BF16;
-  switch (head_dim) {
-    case 64: return bf ? oq::launch_prompt<true, 64, 1, 64>(a, s) : oq::launch_prompt<false, 64, 1, 64>(a, s);
-    case 128: return bf ? oq::launch_prompt<true, 128, 1, 64>(a, s) : oq::launch_prompt<false, 128, 1, 64>(a, s);
-    default: return bf ? oq::launch_prompt<true, 256, 1, 32>(a, s) : oq::launch_prompt<false, 256, 1, 32>(a, s);
-  }
+  return dtype == OQ_OUT_BF16 ? oq::launch_prompt_any<true>(a, head_dim, s) : oq::launch_prompt_any<false>(a, head_dim, s);
 }

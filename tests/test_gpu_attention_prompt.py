@@ -59,6 +59,20 @@ def test_heads(hq, hk):
 def test_one_sequence(n):
     _run([n], 2, 1, 128, True, torch.float16, packed=False)
     _run([n], 2, 1, 256, False, torch.bfloat16)
+    _run([n], 2, 1, 64, True, torch.bfloat16)
+
+
+@pytest.mark.parametrize("d", [64, 128, 256])
+@pytest.mark.parametrize("causal", [True, False])
+def test_workgroup_shapes(d, causal):
+    """Every shape of workgroup over several steps: few and many heads, one long
+    sequence and several."""
+    _run([500], 4, 1, d, causal, torch.float16)             # key groups
+    _run([700], 44, 2, d, causal, torch.bfloat16)           # one group, many steps (d = 64: two)
+    _run([300, 290, 310], 12, 3, d, causal, torch.float16)
+    if causal:
+        _run([2100], 20, 1, d, causal, torch.float16)       # few long rows
+
 
 
 def test_many_sequences():
