@@ -129,4 +129,60 @@ constexpr int ring_tiling(int64_t M, int64_t N, int64_t K, bool a8) {
   return best;
 }
 
+// W8A8: whether the small-M kernel takes a product; the ring's 64 x 64 tiles with
+// three buffers are faster from there on.  Weights from HBM, us on the small-M
+// kernel against the ring: 1 x 2560 x 2048 5.4 / 7.4, 16 x 2048 x 8192 10.6 / 16.9, 16 x 5000 x
+// 8192 14.5 / 17.4, 16 x 32768 x 2048 17.0 / 16.8 (at worst 16 x 8200 x 4096 12.4 / 11.4); 17 x 8200
+// x 4096 16.7 / 11.3; 32 x 4096 x 4096 10.1 / 10.7, 40 x 4096 x 4096 10.9 / 10.8.
+constexpr bool w8_few_rows(int64_t M, int64_t N) { return M <= 16 || (M <= 32 && N <= 4096); }
+
+// W8A8 tilings (both operands staged as they are, 128-code stages): 256 x 256 and
+// 128 x 128 of 8 waves, 128 x 64 and 64 x 64 of 4 (the last with three
+// buffers, since few tiles wait for their loads), and 64 x 64 of 8 waves in two K
+// groups with 256-code stages, three buffers and one workgroup a CU.  Costs as
+// kRingCost's; the tiling chosen is within 12% of the fastest at the 25 shapes that the host
+// test holds.  16384 x 8192 x 8192: 920 us, 2390 TOP/s (the library's int8 product of 8192 cubed:
+// 2070); 4096 cubed 67 us.
+constexpr int kTilingsW8 = 5;
+constexpr RingCost kRingCostW8[kTilingsW8] = {{256, 256, 1, 11.5f, 13.7f, 8.0f},
+                                              {128, 128, 2, 4.7f, 4.6f, 4.5f},
+                                              {128, 64, 3, 4.1f, 2.85f, 4.3f},
+                                              {64, 64, 3, 2.35f, 1.66f, 4.0f},
+                                              {64, 64, 1, 1.7f, 1.85f, 4.2f}};
+// (As ring_estimate; a CU with two tiles is not done before a lone one.)
+constexpr float w8_estimate(const RingCost& c, int64_t M, int64_t N, int64_t K) {
+  const float e = ring_estimate(c, M, N, K), lone = c.fixed + 1e-3f * static_cast<float>(K) * c.lat;
+  return e > lone ? e : lone;
+}
+constexpr int w8_tiling(int64_t M, int64_t N, int64_t K) {
+  // (Up to K = 256 as W4A8's: the product is its output's stores.)
+  int best = K <= 256 && ((M + 255) / 256) * ((N + 255) / 256) <= 1280 ? 1 : 0;
+  for (int i = best + 1; i < kTilingsW8; ++i)
+    if (w8_estimate(kRingCostW8[i], M, N, K) < w8_estimate(kRingCostW8[best], M, N, K)) best = i;
+  return best;
+}
+constexpr float w8_best(int64_t M, int64_t N, int64_t K) { return w8_estimate(kRingCostW8[w8_tiling(M, N, K)], M, N, K); }
+
+// A product of 256 x 256 tiles whose last round fills few CUs is taken in two
+// launches: the columns (or rows) of its whole rounds, and the rest on the tiling
+// that suits it.  4000 x 8200 x 8192 (33 columns of tiles in rounds of 16 x 16): 309 -> 253 us;
+// 9000 x 5000 x 1024, one launch, 67.  at: where the second part begins (0: one launch).
+struct W8Split {
+  bool columns;
+  int64_t at;
+};
+constexpr W8Split w8_split(int64_t M, int64_t N, int64_t K) {
+  W8Split s{true, 0};
+  const int64_t tm = (M + 255) / 256, tn = (N + 255) / 256, rounds = tm * tn / 256;
+  if (rounds < 1) return s;
+  float best = 0.92f * w8_best(M, N, K);
+  const int64_t n1 = rounds * 256 / tm * 256, m1 = rounds * 256 / tn * 256;
+  if (n1 > 0 && n1 < N && w8_tiling(M, n1, K) == 0 && w8_best(M, n1, K) + w8_best(M, N - n1, K) < best) {
+    best = w8_best(M, n1, K) + w8_best(M, N - n1, K);
+    s = W8Split{true, n1};
+  }
+  if (m1 > 0 && m1 < M && w8_tiling(m1, N, K) == 0 && w8_best(m1, N, K) + w8_best(M - m1, N, K) < best) s = W8Split{false, m1};
+  return s;
+}
+
 }  // namespace oq

@@ -20,7 +20,7 @@
 // Other M <= 64 (and token codes in the 16-row tiled layout): a weight-streaming kernel on
 // v_mfma_i32_16x16x64_i8 with the operands loaded straight into registers
 // (details at gemm_small_kernel).  8-bit token codes (W4A8) use both with
-// the A operand loaded as bytes.
+// the A operand loaded as bytes; with 8-bit weights too (W8A8) nothing is widened.
 #include "common.h"
 #include "gemm_ring.h"
 #include "gemm_rules.h"
@@ -375,8 +375,49 @@ int launch_ring(const GemmArgs& a, Epilogue epi, hipStream_t stream) {
   return launch_status();
 }
 
+// W8A8 (no fused epilogue of the DiT takes it).
+int launch_w8(const GemmArgs& a, Epilogue epi, hipStream_t stream) {
+  if (epi != EPI_I32 && epi != EPI_F16 && epi != EPI_BF16) return OQ_ERR_ARG;
+  if (w8_few_rows(a.M, a.N)) {
+    switch (epi) {
+      case EPI_I32: return launch_small_any<EPI_I32>(a, stream);
+      case EPI_F16: return launch_small_any<EPI_F16>(a, stream);
+      default: return launch_small_any<EPI_BF16>(a, stream);
+    }
+  }
+  const W8Split sp = w8_split(a.M, a.N, a.K);
+  if (sp.at > 0) {
+    const int64_t size = epi == EPI_I32 ? 4 : 2;
+    GemmArgs x = a, y = a;
+    if (sp.columns) {
+      x.N = sp.at;
+      y.N = a.N - sp.at;
+      y.B = a.B + sp.at * a.K;
+      y.ws = a.ws ? a.ws + sp.at : nullptr;
+      y.bias = a.bias ? a.bias + sp.at : nullptr;
+      y.C = static_cast<uint8_t*>(a.C) + sp.at * size;
+    } else {
+      x.M = sp.at;
+      y.M = a.M - sp.at;
+      y.A = a.A + sp.at * a.K;
+      y.xs = a.xs ? a.xs + sp.at : nullptr;
+      y.C = static_cast<uint8_t*>(a.C) + sp.at * a.ldc * size;
+    }
+    const int st = launch_w8(x, epi, stream);
+    return st != OQ_OK ? st : launch_w8(y, epi, stream);
+  }
+  switch (w8_tiling(a.M, a.N, a.K)) {
+    case 0: return launch_ring<2, 4, 4, 2, false, 8, 2, 1, 4, true>(a, epi, stream);
+    case 1: return launch_ring<2, 4, 2, 1, false, 8, 2, 1, 1, true>(a, epi, stream);
+    case 2: return launch_ring<2, 2, 2, 1, false, 8, 2, 1, 1, true>(a, epi, stream);
+    case 3: return launch_ring<2, 2, 1, 1, false, 8, 3, 1, 1, true>(a, epi, stream);
+    default: return launch_ring<2, 2, 1, 1, false, 16, 3, 2, 1, true>(a, epi, stream);
+  }
+}
+
 int gemm_launch(const GemmArgs& a, Epilogue epi, hipStream_t stream) {
   if (a.M == 0) return OQ_OK;
+  if (a.b_i8) return launch_w8(a, epi, stream);
   if (a.a_i8 && (epi == EPI_RESID_F32 || epi == EPI_GELU_F16)) return OQ_ERR_ARG;
   if (few_rows(a.M, a.N, a.K, a.a_i8, a.a_tiled)) {
     switch (epi) {
@@ -386,13 +427,6 @@ int gemm_launch(const GemmArgs& a, Epilogue epi, hipStream_t stream) {
       case EPI_RESID_F32: return launch_small_any<EPI_RESID_F32>(a, stream);
       case EPI_GELU_F16: return launch_small_any<EPI_GELU_F16>(a, stream);
       default: return OQ_ERR_ARG;
-    }
-  }
-  if (a.b_i8) {
-    switch (ring_tiling(a.M, a.N, a.K, true)) {
-      case 0: return launch_ring<2, 4, 4, 2, false, 8, 2, 1, 4, true>(a, epi, stream);
-      case 1: return launch_ring<2, 2, 2, 2, false, 8, 2, 1, 1, true>(a, epi, stream);
-      default: return launch_ring<1, 2, 2, 1, false, 8, 2, 2, 1, true>(a, epi, stream);
     }
   }
   if (a.a_i8) {

@@ -14,7 +14,8 @@ DEV = torch.device("cuda:0")
 CASES = [
     (1, 2560, 2048), (1, 64, 64), (16, 2048, 16384), (17, 200, 2048), (50, 3000, 1024), (50, 8192, 1024), (40, 9000, 2048),
     (64, 520, 4160), (3, 100, 64), (65, 320, 1536), (130, 1000, 1024), (256, 4096, 4096), (1000, 2048, 2112), (50, 1024, 4096),
-    (700, 4104, 192), (129, 257, 320), (2000, 2056, 704), (300, 8200, 64), (64, 20000, 128), (5, 33000, 1088),
+    (700, 4104, 192), (129, 257, 320), (2000, 2056, 704), (300, 8200, 64), (64, 20000, 128), (5, 33000, 1088), (20, 520, 4160),
+    (1000, 4096, 320), (3000, 3000, 1024), (4100, 4096, 1024), (4096, 4104, 1024),
 ]
 
 
