@@ -620,7 +620,8 @@ int oq_kv4_gather(const oq_kv4_cache* cache, const int64_t* slots, int64_t n, vo
  * sees no key gives zeros.  One token per sequence is decoding; several are a
  * chunk of a prompt or a draft to verify.
  * Q        device fp16 / bf16 (dtype) [tokens][ldq], head h at columns h d ..;
- *          ldq >= n_heads d, % 8 == 0, 16-byte aligned.  O likewise (dtype, ldo)
+ *          ldq >= n_heads d, % 8 == 0, 16-byte aligned.  O likewise (dtype, ldo); O may
+ *          not overlap Q or the cache
  * cu_q     device int32 [n_seqs + 1]: sequence b's query tokens are rows
  *          cu_q[b] .. cu_q[b + 1] - 1; NULL: one each (tokens == n_seqs,
  *          max_q == 1).  Rows that no sequence has, and those past the first
@@ -629,7 +630,7 @@ int oq_kv4_gather(const oq_kv4_cache* cache, const int64_t* slots, int64_t n, vo
  * block_table  device int32 [n_seqs][table_ld]: page of each page_tokens tokens
  *          of a sequence; tokens of an entry out of range are masked
  * seq_lens device int32 [n_seqs]; clamped to [0, max_len]
- * max_len  >= 0, at least the longest sequence; table_ld page_tokens >= max_len.
+ * max_len  0 .. 2^30, at least the longest sequence; table_ld page_tokens >= max_len.
  *          It plans the split over the length: a tight one is faster.
  * scale    > 0, finite
  * work     device, 16-byte aligned, at least oq_attention_kv4_workspace_bytes(the

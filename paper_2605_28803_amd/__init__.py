@@ -300,15 +300,26 @@ def quantize_weights_i8(W_u, had_block, Wq8=None, w_scale=None, stream=None):
     return Wq8, w_scale
 
 
+def _int8_operands(Xq8, Wq8):
+    if (Xq8.dtype != torch.int8 or Wq8.dtype != torch.int8 or Wq8.shape[1] != Xq8.shape[1] or not Xq8.is_contiguous()
+            or not Wq8.is_contiguous()):
+        raise ValueError("Xq8 and Wq8: contiguous int8 [M, K] and [N, K] expected")
+
+
 def w8a8_linear(Xq8, x_scale, Wq8, w_scale, bias=None, out_dtype=OUT_F16, Y=None, stream=None):
     """Y [M, N] = dequant(Xq8 . Wq8^T) with 8-bit codes on both sides (int8 [M, K], [N, K])."""
     M, K = Xq8.shape
     N = Wq8.shape[0]
-    if Wq8.shape[1] != K or Xq8.dtype != torch.int8 or Wq8.dtype != torch.int8:
-        raise ValueError("Xq8 and Wq8: int8 [M, K] and [N, K] expected")
+    _int8_operands(Xq8, Wq8)
+    if x_scale.numel() != M or w_scale.numel() != N or x_scale.dtype != torch.float32 or w_scale.dtype != torch.float32:
+        raise ValueError("x_scale and w_scale: float32 [M] and [N] expected")
+    if bias is not None and (bias.numel() != N or bias.dtype != torch.float16):
+        raise ValueError("bias: float16 [N] expected")
+    dt = torch.float16 if out_dtype == OUT_F16 else torch.bfloat16
     if Y is None:
-        dt = torch.float16 if out_dtype == OUT_F16 else torch.bfloat16
         Y = torch.empty((M, N), dtype=dt, device=Xq8.device)
+    elif Y.shape != (M, N) or Y.dtype != dt or (N > 1 and Y.stride(1) != 1):
+        raise ValueError("Y: [M, N] rows of out_dtype expected")
     _check(lib().oq_w8a8_linear(_ptr(Xq8), _ptr(x_scale), M, _ptr(Wq8), _ptr(w_scale), _ptr(bias), N, K,
                                 _ptr(Y), _ld(Y), out_dtype, _stream(stream)), "oq_w8a8_linear")
     return Y
@@ -317,10 +328,11 @@ def w8a8_linear(Xq8, x_scale, Wq8, w_scale, bias=None, out_dtype=OUT_F16, Y=None
 def w8a8_gemm_i32(Xq8, Wq8, acc=None, stream=None):
     M, K = Xq8.shape
     N = Wq8.shape[0]
-    if Wq8.shape[1] != K or Xq8.dtype != torch.int8 or Wq8.dtype != torch.int8:
-        raise ValueError("Xq8 and Wq8: int8 [M, K] and [N, K] expected")
+    _int8_operands(Xq8, Wq8)
     if acc is None:
         acc = torch.empty((M, N), dtype=torch.int32, device=Xq8.device)
+    elif acc.shape != (M, N) or acc.dtype != torch.int32 or (N > 1 and acc.stride(1) != 1):
+        raise ValueError("acc: int32 [M, N] rows expected")
     _check(lib().oq_w8a8_gemm_i32(_ptr(Xq8), M, _ptr(Wq8), N, K, _ptr(acc), _ld(acc), _stream(stream)),
            "oq_w8a8_gemm_i32")
     return acc

@@ -10,8 +10,9 @@ import ctypes as C
 
 import torch
 
-from . import _check, _lib, _ptr, _stream  # (the package has these before it imports this module)
+from . import _check, _lib, _ptr, _raw_stream, _stream  # (the package has these before it imports this module)
 
+_current_device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
 _DTYPE = {torch.float16: 0, torch.bfloat16: 1, torch.float32: 2}
 _TORCH = {0: torch.float16, 1: torch.bfloat16, 2: torch.float32}
 
@@ -23,15 +24,17 @@ def _want(ok, what):
 
 # The host's time bounds the smallest calls, so the checks below ask a tensor as little as they can.
 
-def _heads(t, name, head_dim=None):
+def _heads(t, name, head_dim):
     """Token stride of a [tokens, heads, head_dim] tensor whose heads of a token
     lie side by side."""
-    _want(t.dim() == 3, f"{name}: [tokens, heads, head_dim] expected")
-    n, h, d = t.shape
-    _want(head_dim is None or d == head_dim, f"{name}: [tokens, heads, head_dim] expected")
-    s0, s1, s2 = t.stride()
-    _want((s2 == 1 or d <= 1) and (s1 == d or h <= 1), f"{name}: the heads of a token must lie side by side")
-    return s0 if n > 1 else h * d
+    if t.dim() == 3:
+        n, h, d = t.shape
+        s0, s1, s2 = t.stride()
+        if d == head_dim:
+            if s2 == 1 and (s1 == d or h <= 1):
+                return s0 if n > 1 else h * d
+            raise ValueError(f"{name}: the heads of a token must lie side by side")
+    raise ValueError(f"{name}: [tokens, heads, head_dim] expected")
 
 
 def _ints(t, name, dtype, n, dev):
@@ -39,13 +42,19 @@ def _ints(t, name, dtype, n, dev):
         raise ValueError(f"{name}: contiguous {dtype} of {n} elements on cuda:{dev} expected")
 
 
-def _device(t, *others):
+def _device(t, u, v):
     """Index of the tensors' device, which has to be the current one (the library
     launches there)."""
     dev = t.get_device()
-    _want(dev >= 0 and all(o.get_device() == dev for o in others), "the tensors must be on one GPU")
-    _want(dev == torch.cuda.current_device(), f"cuda:{dev} is not the current device")
+    if dev < 0 or u.get_device() != dev or v.get_device() != dev:
+        raise ValueError("the tensors must be on one GPU")
+    if dev != _current_device():
+        raise ValueError(f"cuda:{dev} is not the current device")
     return dev
+
+
+def _on(stream, dev):
+    return _raw_stream(dev) if stream is None and _raw_stream is not None else _stream(stream)
 
 
 def attention_prompt(Q, K, V, cu_seqlens, causal=True, scale=None, O=None, stream=None):
@@ -53,8 +62,9 @@ def attention_prompt(Q, K, V, cu_seqlens, causal=True, scale=None, O=None, strea
     Q [T, Hq, d], K, V [T, Hkv, d] fp16 or bf16 (views of a q|k|v output serve),
     cu_seqlens int32 [n + 1] on the device; scale defaults to d ** -0.5.  Rows of
     no sequence are left as they were in O (unspecified when O is made here)."""
-    ldq, ldk, ldv = _heads(Q, "Q"), _heads(K, "K", Q.shape[2]), _heads(V, "V", Q.shape[2])
+    _want(Q.dim() == 3, "Q: [tokens, heads, head_dim] expected")
     T, hq, d = Q.shape
+    ldq, ldk, ldv = _heads(Q, "Q", d), _heads(K, "K", d), _heads(V, "V", d)
     dev = _device(Q, K, V)
     _want(K.shape[0] == T and V.shape == K.shape, "K and V need Q's tokens and equal shapes")
     _want(Q.dtype in _DTYPE and K.dtype == Q.dtype and V.dtype == Q.dtype, "Q, K and V need one type")
@@ -62,13 +72,13 @@ def attention_prompt(Q, K, V, cu_seqlens, causal=True, scale=None, O=None, strea
     _want(n_cu >= 1, "cu_seqlens: at least one element expected")
     _ints(cu_seqlens, "cu_seqlens", torch.int32, n_cu, dev)
     if O is None:
-        O, ldo = torch.empty((T, hq, d), dtype=Q.dtype, device=Q.device), hq * d
+        O, ldo = Q.new_empty((T, hq, d)), hq * d
     else:
         _want(O.shape == Q.shape and O.dtype == Q.dtype and O.get_device() == dev, "O: Q's shape, type and device expected")
-        ldo = _heads(O, "O")
+        ldo = _heads(O, "O", d)
     _check(_lib.load().oq_attention_prompt(_ptr(Q), _ptr(K), _ptr(V), T, ldq, ldk, ldv, _DTYPE[Q.dtype], _ptr(cu_seqlens),
                                            n_cu - 1, hq, K.shape[1], d, int(causal),
-                                           d ** -0.5 if scale is None else scale, _ptr(O), ldo, _stream(stream)),
+                                           d ** -0.5 if scale is None else scale, _ptr(O), ldo, _on(stream, dev)),
            "oq_attention_prompt")
     return O
 
@@ -95,6 +105,7 @@ class KV4Cache:
         self._c = _lib.oq_kv4_cache(k_codes.data_ptr(), v_codes.data_ptr(), k_scale.data_ptr(), v_scale.data_ptr(), p, t, h,
                                     2 * half, int(self.rotate_k))
         self.ref = C.byref(self._c)
+        self._work_bytes = {}  # workspace sizes asked for (of this cache's heads)
 
     @classmethod
     def empty(cls, n_pages, n_kv_heads, head_dim, page_tokens=64, rotate_k=True, device="cuda:0"):
@@ -115,7 +126,7 @@ def kv4_append(cache, K, V, slots, stream=None):
     _want(K.shape[1] == cache.n_kv_heads and V.shape == K.shape, "K and V: [n, the cache's heads, head_dim] expected")
     _want(K.dtype in _DTYPE and V.dtype == K.dtype, "K and V need one type")
     _ints(slots, "slots", torch.int64, n, dev)
-    _check(_lib.load().oq_kv4_append(cache.ref, _ptr(K), _ptr(V), n, ldk, ldv, _DTYPE[K.dtype], _ptr(slots), _stream(stream)),
+    _check(_lib.load().oq_kv4_append(cache.ref, _ptr(K), _ptr(V), n, ldk, ldv, _DTYPE[K.dtype], _ptr(slots), _on(stream, dev)),
            "oq_kv4_append")
 
 
@@ -123,7 +134,7 @@ def kv4_gather(cache, slots, out_dtype=0, K=None, V=None, stream=None):
     """(K, V) [n, Hkv, d]: the values that the slots hold (fp16, bf16 or fp32 by
     out_dtype: OUT_F16, OUT_BF16, OUT_F32)."""
     n = slots.numel()
-    dev = _device(slots, cache.k_codes)
+    dev = _device(slots, slots, cache.k_codes)
     _ints(slots, "slots", torch.int64, n, dev)
     dt = _TORCH.get(out_dtype)
     _want(dt is not None, "out_dtype: OUT_F16, OUT_BF16 or OUT_F32 expected")
@@ -134,16 +145,22 @@ def kv4_gather(cache, slots, out_dtype=0, K=None, V=None, stream=None):
             ld.append(shape[1] * shape[2])
         else:
             _want(t.shape == shape and t.dtype == dt and t.get_device() == dev, f"{name}: {list(shape)} of {dt} on cuda:{dev} expected")
-            ld.append(_heads(t, name))
+            ld.append(_heads(t, name, shape[2]))
     K = torch.empty(shape, dtype=dt, device=slots.device) if K is None else K
     V = torch.empty(shape, dtype=dt, device=slots.device) if V is None else V
     _check(_lib.load().oq_kv4_gather(cache.ref, _ptr(slots), n, _ptr(K), _ptr(V), ld[0], ld[1], out_dtype,
-                                     _stream(stream)), "oq_kv4_gather")
+                                     _on(stream, dev)), "oq_kv4_gather")
     return K, V
 
 
 def attention_kv4_workspace_bytes(cache, tokens, n_heads, n_seqs, max_q, max_len) -> int:
-    return int(_lib.load().oq_attention_kv4_workspace_bytes(cache.ref, tokens, n_heads, n_seqs, max_q, max_len))
+    key = (tokens, n_heads, n_seqs, max_q, max_len)
+    size = cache._work_bytes.get(key)
+    if size is None:
+        if len(cache._work_bytes) >= 256:  # (max_len may grow with every step)
+            cache._work_bytes.clear()
+        size = cache._work_bytes[key] = int(_lib.load().oq_attention_kv4_workspace_bytes(cache.ref, *key))
+    return size
 
 
 def attention_kv4(Q, cache, block_table, seq_lens, cu_q=None, max_q=None, max_len=None, causal=True, scale=None, O=None,
@@ -157,7 +174,7 @@ def attention_kv4(Q, cache, block_table, seq_lens, cu_q=None, max_q=None, max_le
     are left as they were in O (unspecified when O is made here)."""
     ldq = _heads(Q, "Q", cache.head_dim)
     T, hq, d = Q.shape
-    dev = _device(Q, cache.k_codes)
+    dev = _device(Q, Q, cache.k_codes)
     n = seq_lens.numel()
     _want(Q.dtype in _DTYPE, "Q: fp16 or bf16 expected")
     _want(block_table.dim() == 2 and block_table.shape[0] == n, "block_table: [sequences, width] expected")
@@ -172,12 +189,12 @@ def attention_kv4(Q, cache, block_table, seq_lens, cu_q=None, max_q=None, max_le
         _want(max_q is not None, "cu_q needs max_q")
         _ints(cu_q, "cu_q", torch.int32, n + 1, dev)
     if max_len is None:
-        max_len = min(width * cache.page_tokens, 2 ** 31 - 1)
+        max_len = min(width * cache.page_tokens, 2 ** 30)
     if O is None:
-        O, ldo = torch.empty((T, hq, d), dtype=Q.dtype, device=Q.device), hq * d
+        O, ldo = Q.new_empty((T, hq, d)), hq * d
     else:
         _want(O.shape == Q.shape and O.dtype == Q.dtype and O.get_device() == dev, "O: Q's shape, type and device expected")
-        ldo = _heads(O, "O")
+        ldo = _heads(O, "O", d)
     if work is None:
         nbytes = attention_kv4_workspace_bytes(cache, T, hq, n, max_q, max_len)
         work = torch.empty((nbytes,), dtype=torch.uint8, device=Q.device) if nbytes else None
@@ -186,5 +203,5 @@ def attention_kv4(Q, cache, block_table, seq_lens, cu_q=None, max_q=None, max_le
     _check(_lib.load().oq_attention_kv4(cache.ref, _ptr(Q), T, ldq, hq, _DTYPE[Q.dtype], _ptr(cu_q), max_q, _ptr(block_table),
                                         width, _ptr(seq_lens), n, max_len, int(causal), d ** -0.5 if scale is None else scale,
                                         _ptr(O), ldo, _ptr(work), 0 if work is None else work.numel(),
-                                        _stream(stream)), "oq_attention_kv4")
+                                        _on(stream, dev)), "oq_attention_kv4")
     return O

@@ -346,19 +346,19 @@ constexpr int kTile = 64;  // tokens of one step of a wave
 
 __device__ __forceinline__ uint32_t and_xor(uint32_t a, uint32_t m, uint32_t x) { return (a & m) ^ x; }
 
-// Rows of the call: query token range of sequence b.
-__device__ __forceinline__ void query_rows(const AttnKv4& a, int b, int& q0, int& nq) {
-  q0 = b;
-  nq = 1;
+// Query tokens of sequence b: the first row, how many of them are computed, and
+// `at`, the place of the first one in a sequence of L tokens (they are its last).
+__device__ __forceinline__ void query_rows(const AttnKv4& a, int b, int L, int& q0, int& nq, int& at) {
+  int64_t lo = b, n = 1;
   if (a.cu_q) {
     const int64_t s = a.cu_q[b], e = a.cu_q[b + 1];
-    const int64_t lo = s < 0 ? 0 : s > a.tokens ? a.tokens : s;
-    int64_t n = e - s;
-    n = n > a.max_q ? a.max_q : n;
-    n = n > a.tokens - lo ? a.tokens - lo : n;
-    q0 = static_cast<int>(lo);
-    nq = n < 0 ? 0 : static_cast<int>(n);
+    lo = s < 0 ? 0 : s > a.tokens ? a.tokens : s;
+    n = e > s ? e - s : 0;
   }
+  q0 = static_cast<int>(lo);
+  at = static_cast<int>(n > INT32_MAX / 2 ? -(INT32_MAX / 2) : L - n);
+  n = n > a.max_q ? a.max_q : n;
+  nq = static_cast<int>(n > a.tokens - lo ? a.tokens - lo : n);
 }
 
 // Softmax lanes.  A tile has 16 columns, but often fewer rows to fill them: with
@@ -438,10 +438,11 @@ __global__ __launch_bounds__(64 * W, QT == 1 ? D < 256 ? 3 : 2 : 1) void attn_kv
   uint32_t in_page;
   int page = entry(first / 16 + g, in_page);
   const int L = __builtin_amdgcn_readfirstlane(max(0, min(a.lens[b], a.max_len)));
-  int q0, nq;
-  query_rows(a, b, q0, nq);
+  int q0, nq, q_at;
+  query_rows(a, b, L, q0, nq, q_at);
   q0 = __builtin_amdgcn_readfirstlane(q0);
   nq = __builtin_amdgcn_readfirstlane(nq);
+  q_at = __builtin_amdgcn_readfirstlane(q_at);
   const int rows = nq * a.R, r0 = blockIdx.x * ROWS;
   // (The first chunk of an empty sequence writes its zeros.)
   if (r0 >= rows || (c0 >= L && split > 0)) return;
@@ -481,10 +482,10 @@ __global__ __launch_bounds__(64 * W, QT == 1 ? D < 256 ? 3 : 2 : 1) void attn_kv
 #pragma unroll
   for (int t = 0; t < QT; ++t) {
     const int r = min(r0 + 16 * t + row_in, rows - 1);
-    seen[t] = a.causal ? max(0, L - nq + 1 + r / a.R) : L;
+    seen[t] = a.causal ? max(0, q_at + 1 + r / a.R) : L;
   }
-  const int all_seen = a.causal ? max(0, L - nq + 1 + r0 / a.R) : L;  // every row sees these
-  const int last_seen = a.causal ? max(0, L - nq + 1 + min(r0 + ROWS - 1, rows - 1) / a.R) : L;
+  const int all_seen = a.causal ? max(0, q_at + 1 + r0 / a.R) : L;  // every row sees these
+  const int last_seen = a.causal ? max(0, q_at + 1 + min(r0 + ROWS - 1, rows - 1) / a.R) : L;
   const int end = min(last_seen, c0 + a.chunk);
 
   // Queries: TQ threads take a row's channels (rotation, power-of-two norm, fp16
@@ -801,8 +802,8 @@ __global__ __launch_bounds__(256) void attn_kv4_join_kernel(AttnKv4 a) {
   const int head = blockIdx.x * RPW + sub, b = blockIdx.z;
   const int L = max(0, min(a.lens[b], a.max_len));
   if (L <= a.chunk) return;
-  int q0, nq;
-  query_rows(a, b, q0, nq);
+  int q0, nq, q_at;
+  query_rows(a, b, L, q0, nq, q_at);
   if (static_cast<int>(blockIdx.y) >= nq) return;
   const int splits = (L + a.chunk - 1) / a.chunk;
   const int64_t tok = q0 + blockIdx.y;
@@ -896,7 +897,7 @@ Kv4Plan kv4_plan(int64_t n_seqs, int hk, int d, int R, int max_q, int64_t max_le
   p.waves = p.qt == 1 && max_len <= kWholeLen && wgs <= 512 ? 8 : 4;
   const int64_t step = p.waves * kTile;
   int64_t chunk = wgs * max_len / kTargetWgs;
-  chunk = chunk < max_len / kMaxSplits ? max_len / kMaxSplits : chunk;
+  chunk = chunk < max_len / kMaxSplits ? max_len / kMaxSplits : chunk > max_len ? max_len : chunk;
   chunk = (chunk + step - 1) / step * step;
   p.chunk = static_cast<int>(chunk < step ? step : chunk);
   p.splits = static_cast<int>(max_len <= p.chunk ? 1 : (max_len + p.chunk - 1) / p.chunk);
@@ -998,7 +999,7 @@ extern "C" int oq_kv4_gather(const oq_kv4_cache* cache, const int64_t* slots, in
 
 static int attn_kv4_shape(const oq_kv4_cache* cache, int64_t tokens, int32_t n_heads, int32_t n_seqs, int32_t max_q,
                           int32_t max_len) {
-  if (tokens < 0 || tokens > INT32_MAX || n_seqs < 0 || max_q < 1 || max_q > 65535 || max_len < 0 || n_heads < 1) return OQ_ERR_SHAPE;
+  if (tokens < 0 || tokens > INT32_MAX || n_seqs < 0 || max_q < 1 || max_q > 65535 || max_len < 0 || max_len > (1 << 30) || n_heads < 1) return OQ_ERR_SHAPE;
   if (n_heads % cache->n_kv_heads != 0) return OQ_ERR_SHAPE;
   if (static_cast<int64_t>(n_seqs) * cache->n_kv_heads > 65535) return OQ_ERR_SHAPE;
   if (static_cast<int64_t>(max_q) * (n_heads / cache->n_kv_heads) > INT32_MAX / 2) return OQ_ERR_SHAPE;

@@ -325,6 +325,27 @@ def test_lengths_past_max_len_are_clamped():
     assert (c == 0).all()
 
 
+def test_query_tokens_past_max_q_are_left():
+    """max_q below a sequence's query tokens: the first max_q are what they are without it."""
+    for n in (900, 3000):
+        cache, table, lens, _ = _small(n=n)
+        q = torch.randn((9, 8, 128), device=DEV, generator=torch.Generator(device=DEV).manual_seed(7)).half()
+        cu = torch.tensor([1, 8], dtype=torch.int32, device=DEV)
+        full = oq.attention_kv4(q, cache, table, lens, cu, max_q=7, max_len=n)
+        O = torch.full_like(q, 3.0)
+        oq.attention_kv4(q, cache, table, lens, cu, max_q=4, max_len=n, O=O)
+        torch.cuda.synchronize()
+        torch.testing.assert_close(O[1:5], full[1:5], rtol=2.0 ** -9, atol=2.0 ** -11)  # (other splits)
+        assert (O[5:] == 3.0).all() and (O[0] == 3.0).all()
+
+
+def test_empty_cache_and_no_table():
+    cache = oq.KV4Cache.empty(1, 2, 64, 16)
+    q = torch.randn((3, 4, 64), device=DEV).half()
+    o = oq.attention_kv4(q, cache, torch.zeros((3, 0), dtype=torch.int32, device=DEV), torch.tensor([0, 5, -1], dtype=torch.int32, device=DEV))
+    assert (o == 0).all()
+
+
 def test_nothing_to_do():
     cache, table, lens, q = _small()
     e = q[:0]

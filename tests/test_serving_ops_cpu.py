@@ -77,7 +77,7 @@ def _attend(lib, cache=None, Q=P16, tokens=4, ldq=1024, heads=8, dtype=0, cu=Non
     (dict(cu=P2), ALIGN), (dict(ldq=1028), ALIGN), (dict(ldo=1028), ALIGN),
     (dict(tokens=-1), SHAPE), (dict(tokens=5), SHAPE), (dict(max_q=2), SHAPE), (dict(max_q=0), SHAPE), (dict(max_q=65536, cu=P16), SHAPE), (dict(heads=7), SHAPE),
     (dict(heads=0), SHAPE), (dict(n=-1), SHAPE), (dict(n=40000, tokens=40000), SHAPE), (dict(max_len=-1), SHAPE),
-    (dict(max_len=513), SHAPE), (dict(table_ld=-1), SHAPE), (dict(ldq=1016), SHAPE), (dict(ldo=8), SHAPE),
+    (dict(max_len=513), SHAPE), (dict(max_len=2 ** 30 + 1, table_ld=2 ** 40), SHAPE), (dict(table_ld=-1), SHAPE), (dict(ldq=1016), SHAPE), (dict(ldo=8), SHAPE),
     (dict(dtype=2), ARG), (dict(dtype=-1), ARG), (dict(causal=2), ARG), (dict(scale=0.0), ARG), (dict(scale=-1.0), ARG),
     (dict(scale=math.inf), ARG), (dict(scale=math.nan), ARG),
     (dict(cu=P16, tokens=2 ** 31), SHAPE),
@@ -164,6 +164,29 @@ def test_binding_refusals():
     i8 = torch.zeros((4, 64), dtype=torch.int8)
     with pytest.raises(ValueError, match="int8"):
         oq.w8a8_linear(i8, torch.ones(4), torch.zeros((8, 32), dtype=torch.uint8), torch.ones(8))
+    w8 = torch.zeros((8, 64), dtype=torch.int8)
+    for bad, what in (((i8.t().contiguous().t(), torch.ones(4), w8, torch.ones(8)), "int8"),
+                      ((i8, torch.ones(3), w8, torch.ones(8)), "x_scale"), ((i8, torch.ones(4), w8, torch.ones(9)), "w_scale"),
+                      ((i8, torch.ones(4).half(), w8, torch.ones(8)), "x_scale"),
+                      ((i8, torch.ones(4), w8, torch.ones(8), torch.zeros(8)), "bias"),
+                      ((i8, torch.ones(4), w8, torch.ones(8), None, oq.OUT_F16, torch.zeros((4, 8))), "Y")):
+        with pytest.raises(ValueError, match=what):
+            oq.w8a8_linear(*bad)
+    with pytest.raises(ValueError, match="acc"):
+        oq.w8a8_gemm_i32(i8, w8, torch.zeros((4, 9), dtype=torch.int32))
+
+
+@pytest.mark.parametrize("cache", [dict(n_kv_heads=1, head_dim=64), dict(n_kv_heads=8, head_dim=128), dict(n_kv_heads=2, head_dim=256)])
+def test_workspace_holds_every_split(lib, cache):
+    """At most 64 splits of at least 256 tokens, for any plan of the sizes allowed."""
+    c = _c(n_pages=2 ** 20, **cache)
+    hk = cache["n_kv_heads"]
+    for n_seqs in (1, 7, 65535 // hk):
+        for max_q in (1, 50, 65535):
+            for max_len in (1, 512, 513, 131000, 2 ** 30):
+                row = 8 * hk * (cache["head_dim"] + 4) * 4
+                size = lib.oq_attention_kv4_workspace_bytes(c, 3, 8 * hk, n_seqs, max_q, max_len)
+                assert size % (3 * row) == 0 and size // (3 * row) <= min(65, -(-max_len // 256))
 
 
 def test_plain_cache_by_hand():
