@@ -37,7 +37,9 @@ size (the counter calibration reference); --gr00t-only times just the
 GR00T-shaped step; --composite-only times just the full composite rotation;
 --static-only times the static per-channel step path and its calibration;
 --w4a8-only times the W4A8 mode beside W4A4; --prepare-only times the GPU
-weight preparation for the composite rotation.
+weight preparation for the composite rotation; --backbone-only times a
+backbone layer's operators (linears in W4A4 and W8A8, attention over the
+prompt, the 4-bit key/value cache) for a prompt and for one decoded token.
 """
 from __future__ import annotations
 
@@ -645,6 +647,67 @@ def prefill_linears():
     return out
 
 
+def backbone_layer(seqs=1, tokens=None):
+    """The operators of one Gemma-2B-shaped backbone layer, each in a HIP
+    graph of its own (weights and cache warm): for a prompt of 816 tokens the
+    four rotate-quantize + linear pairs in W4A4 and in W8A8, attention over
+    the prompt (8 query heads on one of 256, every token seeing all) and the
+    append to the 4-bit cache; for one decoded token the same with attention
+    over the cached prompt.  Norms, rotary embedding and the activation are
+    not part of the library and not timed."""
+    import torch
+    import paper_2605_28803_amd as oq
+    from workloads import configs
+    cfg = configs.PREFILL_GEMMA
+    dev = torch.device("cuda:0")
+    T = cfg.tokens if tokens is None else tokens
+    hd = cfg.kv_dim
+    hq = cfg.hidden // hd
+    g = torch.Generator(device=dev).manual_seed(11)
+    page = 64
+    pages = -(-(T + 1) // page)
+    cache = oq.KV4Cache.empty(seqs * pages, 1, hd, page, rotate_k=True, device=dev)
+    table = torch.arange(seqs * pages, dtype=torch.int32, device=dev).view(seqs, pages)
+    weights = {}
+    for name, K, N in cfg.linears():
+        W = (torch.randn((N, K), generator=g, device=dev) * cfg.w_std).half()
+        weights[name] = (K, oq.quantize_weights(W, K), oq.quantize_weights_i8(W, K))
+        del W
+    out = {}
+    for what, n in (("prompt", seqs * T), ("token", seqs)):
+        rec = {}
+        for name, (K, w4, w8) in weights.items():
+            X = torch.randn((n, K), generator=g, device=dev).half()
+            for mode, rq, linear, w in (("w4a4", oq.rotate_quantize_act, oq.w4a4_linear, w4),
+                                        ("w8a8", oq.rotate_quantize_act_i8, oq.w8a8_linear, w8)):
+                def pair():
+                    Xq, xs = rq(X, K)
+                    return linear(Xq, xs, *w)
+                rec[f"{name}_{mode}_us"] = round(_graph_time(pair) * 1e3, 2)
+            del X
+        qkv = torch.randn((n, hq + 2, hd), generator=g, device=dev).half()
+        q, k, v = qkv[:, :hq], qkv[:, hq:hq + 1], qkv[:, hq + 1:]
+        row = torch.arange(n, device=dev)
+        if what == "prompt":
+            cu = torch.arange(seqs + 1, dtype=torch.int32, device=dev) * T
+            slots = (row // T) * pages * page + row % T
+            rec["append_us"] = round(_graph_time(lambda: oq.kv4_append(cache, k, v, slots)) * 1e3, 2)
+            t = _graph_time(lambda: oq.attention_prompt(q, k, v, cu, causal=False))
+            rec["attention_TFLOPs"] = round(4 * seqs * T * T * hq * hd / t / 1e9, 1)
+        else:
+            slots = row * pages * page + T
+            lens = torch.full((seqs,), T + 1, dtype=torch.int32, device=dev)
+            rec["append_us"] = round(_graph_time(lambda: oq.kv4_append(cache, k, v, slots)) * 1e3, 2)
+            t = _graph_time(lambda: oq.attention_kv4(q, cache, table, lens, max_len=T + 1))
+        rec["attention_us"] = round(t * 1e3, 2)
+        for mode in ("w4a4", "w8a8"):
+            rec[f"layer_{mode}_us"] = round(sum(rec[f"{name}_{mode}_us"] for name in weights) + rec["append_us"] + rec["attention_us"], 1)
+        out[what] = rec
+    out["tokens"], out["seqs"] = T, seqs
+    out["cache_bytes_per_token"], out["fp16_bytes_per_token"] = hd + 8, 4 * hd
+    return out
+
+
 def pi_step_without_graph(cfg, inp, steps=20):
     """The same Pi-0.5-shaped step launched kernel by kernel (no HIP graph)."""
     import torch
@@ -1105,6 +1168,7 @@ def main():
     ap.add_argument("--static-only", action="store_true")
     ap.add_argument("--w4a8-only", action="store_true")
     ap.add_argument("--prepare-only", action="store_true")
+    ap.add_argument("--backbone-only", action="store_true")
     ap.add_argument("--cpu-kernels-only", action="store_true")
     ap.add_argument("--gemm-prefill-only", action="store_true")
     args = ap.parse_args()
@@ -1127,6 +1191,9 @@ def main():
         print(json.dumps({"w4a8": w4a8_kernels()}), flush=True)
     elif args.prepare_only:
         print(json.dumps({"weight_preparation": prepare_kernels()}), flush=True)
+    elif args.backbone_only:
+        for seqs in (1, 32):
+            print(json.dumps({"backbone_layer": backbone_layer(seqs)}), flush=True)
     elif args.gemm_prefill_only:
         for rec in prefill_gemms():
             print(json.dumps(rec), flush=True)
