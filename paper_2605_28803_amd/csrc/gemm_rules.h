@@ -133,7 +133,8 @@ constexpr int ring_tiling(int64_t M, int64_t N, int64_t K, bool a8) {
 // three buffers are faster from there on.  Weights from HBM, us on the small-M
 // kernel against the ring: 1 x 2560 x 2048 5.4 / 7.4, 16 x 2048 x 8192 10.6 / 16.9, 16 x 5000 x
 // 8192 14.5 / 17.4, 16 x 32768 x 2048 17.0 / 16.8 (at worst 16 x 8200 x 4096 12.4 / 11.4); 17 x 8200
-// x 4096 16.7 / 11.3; 32 x 4096 x 4096 10.1 / 10.7, 40 x 4096 x 4096 10.9 / 10.8.
+// x 4096 13.5 / 11.3; 17 x 2048 x 16384 19.8 / 29.3, 32 x 2048 x 16384 24.6 / 29.3 (two row blocks a workgroup;
+// with four, of which two are empty, 28.3), 40 x 4096 x 4096 10.9 / 10.8.
 constexpr bool w8_few_rows(int64_t M, int64_t N) { return M <= 16 || (M <= 32 && N <= 4096); }
 
 // W8A8 tilings (both operands staged as they are, 128-code stages): 256 x 256 and

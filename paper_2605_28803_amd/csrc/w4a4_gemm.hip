@@ -332,7 +332,7 @@ int launch_small_any(const GemmArgs& a, hipStream_t stream) {
     if constexpr (EPI == EPI_RESID_F32 || EPI == EPI_GELU_F16) return OQ_ERR_ARG;  // DiT paths only
     else
       return a.M <= 16 ? launch_small_mb<EPI, false, 1, true, true>(a, stream)
-                       : launch_small_mb<EPI, false, 4, true, true>(a, stream);
+                       : launch_small_mb<EPI, false, 2, true, true>(a, stream);  // (at most 32 rows; w8_few_rows)
   }
   if (a.a_i8)
     return a.M <= 16 ? launch_small_mb<EPI, false, 1, true>(a, stream) : launch_small_mb<EPI, false, 4, true>(a, stream);

@@ -62,8 +62,8 @@ def test_rule_takes_a_fast_tiling(rules, M, N, K, us):
 
 # (M, N, K, us on the small-M kernel, us on the ring), measured as above.
 FEW = [(1, 2560, 2048, 5.36, 7.36), (1, 16384, 16384, 53.0, 58.3), (8, 8192, 1024, 5.34, 6.28), (16, 2048, 8192, 10.6, 16.9),
-       (16, 5000, 8192, 14.5, 17.4), (16, 32768, 4096, 33.5, 34.9), (17, 8200, 4096, 16.7, 11.3), (17, 32768, 2048, 24.1, 16.9),
-       (17, 4096, 16384, 26.8, 33.2), (32, 2560, 2048, 6.94, 7.53), (32, 4096, 4096, 10.1, 10.7), (40, 4096, 4096, 10.88, 10.81),
+       (16, 5000, 8192, 14.5, 17.4), (16, 32768, 4096, 33.5, 34.9), (17, 8200, 4096, 13.5, 11.1), (17, 32768, 2048, 19.1, 17.3),
+       (17, 2048, 16384, 19.8, 29.3), (32, 2560, 2048, 6.41, 7.61), (32, 4096, 4096, 9.2, 10.7), (32, 2048, 16384, 24.6, 29.3), (40, 4096, 4096, 10.88, 10.81),
        (48, 2048, 8192, 18.8, 16.9), (64, 32768, 2048, 31.8, 19.2), (20, 8192, 1536, 7.69, 7.13)]
 
 
