@@ -428,10 +428,13 @@ int oq_w8a8_gemm_i32(const int8_t* Xq8, int64_t M, const int8_t* Wq8, int64_t N,
  *          cu_seqlens[s] .. cu_seqlens[s + 1] - 1 (clamped to [0, tokens]); rows
  *          of no sequence are left as they were, and what they hold is not used
  * head_dim d: 64, 128 or 256;  n_heads a multiple of n_kv_heads, n_heads <= 65535
- * scale    > 0, finite
+ * scale    > 0, scale log2(e) finite
  * O        device [tokens][ldo] of dtype, ldo % 8 == 0; may not overlap Q, K, V
- * Probabilities are rounded to dtype for the second product; sums and
- * statistics are fp32.  Inputs are finite.
+ * Probabilities are rounded to dtype for the second product (fp16: normal numbers
+ * down to 2^-29 of a row's largest); sums and statistics are fp32.  Q, K and V of the
+ * sequences' rows are finite: one that is not may show in any row of its sequence,
+ * and in no other sequence.  About tokens / 128 + n_seqs workgroups a head, of 2^32
+ * threads at most together (OQ_ERR_SHAPE).
  * Errors: OQ_ERR_NULL, OQ_ERR_SHAPE, OQ_ERR_ALIGN, OQ_ERR_ARG, OQ_ERR_DEVICE,
  * OQ_ERR_HIP.
  */
@@ -632,14 +635,15 @@ int oq_kv4_gather(const oq_kv4_cache* cache, const int64_t* slots, int64_t n, vo
  * seq_lens device int32 [n_seqs]; clamped to [0, max_len]
  * max_len  0 .. 2^30, at least the longest sequence; table_ld page_tokens >= max_len.
  *          It plans the split over the length: a tight one is faster.
- * scale    > 0, finite
+ * scale    > 0, scale log2(e) finite
  * work     device, 16-byte aligned, at least oq_attention_kv4_workspace_bytes(the
  *          same sizes) bytes (0: may be NULL), written before it is read;
  *          calls that share it must not overlap
- * n_seqs n_kv_heads <= 65535.  Keys, steps and values past a sequence's end are
- * not used, whatever they hold.  Queries are used as fp16 times a power of two
- * (rotated ones as two such parts), probabilities as fp16 relative to the
- * largest contribution, sums and statistics in fp32.
+ * n_seqs n_kv_heads <= 65535, n_heads <= 65535, max_q n_heads / n_kv_heads <= 2^26.
+ * Keys, steps and values past a sequence's end are not used, whatever they hold.
+ * Queries are used as fp16 times a power of two (rotated ones as two such parts),
+ * probabilities as fp16 relative to the largest contribution (normal numbers down to
+ * 2^-29 of it), sums and statistics in fp32.
  * Errors: OQ_ERR_NULL, OQ_ERR_SHAPE, OQ_ERR_ALIGN, OQ_ERR_ARG,
  * OQ_ERR_WORKSPACE, OQ_ERR_DEVICE, OQ_ERR_HIP.
  */

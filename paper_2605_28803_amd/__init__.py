@@ -37,6 +37,7 @@ def _check(status: int, where: str):
 # pointers (the prototypes convert them): a call's host time bounds the smallest linears
 # (64 x 1024 x 1024, two calls: 16.1 us with Stream and c_void_p objects, 11.0 us without).
 _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+_current_device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
 
 
 def _stream(stream=None):
@@ -45,6 +46,11 @@ def _stream(stream=None):
     if _raw_stream is None:
         return torch.cuda.current_stream().cuda_stream
     return _raw_stream(torch.cuda.current_device())
+
+
+def _on(stream, dev):
+    """_stream on a device that is known to be the current one."""
+    return _raw_stream(dev) if stream is None and _raw_stream is not None else _stream(stream)
 
 
 def _ld(t):
@@ -306,22 +312,35 @@ def _int8_operands(Xq8, Wq8):
         raise ValueError("Xq8 and Wq8: contiguous int8 [M, K] and [N, K] expected")
 
 
+def _one_gpu(t, *more):
+    """Index of the tensors' device, which has to be the current one (the library
+    launches there)."""
+    dev = t.get_device()
+    if dev < 0 or any([u.get_device() != dev for u in more]):
+        raise ValueError("the tensors must be on one GPU")
+    if dev != _current_device():
+        raise ValueError(f"cuda:{dev} is not the current device")
+    return dev
+
+
 def w8a8_linear(Xq8, x_scale, Wq8, w_scale, bias=None, out_dtype=OUT_F16, Y=None, stream=None):
     """Y [M, N] = dequant(Xq8 . Wq8^T) with 8-bit codes on both sides (int8 [M, K], [N, K])."""
     M, K = Xq8.shape
     N = Wq8.shape[0]
     _int8_operands(Xq8, Wq8)
-    if x_scale.numel() != M or w_scale.numel() != N or x_scale.dtype != torch.float32 or w_scale.dtype != torch.float32:
-        raise ValueError("x_scale and w_scale: float32 [M] and [N] expected")
-    if bias is not None and (bias.numel() != N or bias.dtype != torch.float16):
-        raise ValueError("bias: float16 [N] expected")
+    if (x_scale.numel() != M or w_scale.numel() != N or x_scale.dtype != torch.float32 or w_scale.dtype != torch.float32
+            or not x_scale.is_contiguous() or not w_scale.is_contiguous()):
+        raise ValueError("x_scale and w_scale: contiguous float32 [M] and [N] expected")
+    if bias is not None and (bias.numel() != N or bias.dtype != torch.float16 or not bias.is_contiguous()):
+        raise ValueError("bias: contiguous float16 [N] expected")
     dt = torch.float16 if out_dtype == OUT_F16 else torch.bfloat16
     if Y is None:
         Y = torch.empty((M, N), dtype=dt, device=Xq8.device)
     elif Y.shape != (M, N) or Y.dtype != dt or (N > 1 and Y.stride(1) != 1):
         raise ValueError("Y: [M, N] rows of out_dtype expected")
+    dev = _one_gpu(Xq8, x_scale, Wq8, w_scale, Y) if bias is None else _one_gpu(Xq8, x_scale, Wq8, w_scale, Y, bias)
     _check(lib().oq_w8a8_linear(_ptr(Xq8), _ptr(x_scale), M, _ptr(Wq8), _ptr(w_scale), _ptr(bias), N, K,
-                                _ptr(Y), _ld(Y), out_dtype, _stream(stream)), "oq_w8a8_linear")
+                                _ptr(Y), _ld(Y), out_dtype, _on(stream, dev)), "oq_w8a8_linear")
     return Y
 
 
@@ -333,7 +352,8 @@ def w8a8_gemm_i32(Xq8, Wq8, acc=None, stream=None):
         acc = torch.empty((M, N), dtype=torch.int32, device=Xq8.device)
     elif acc.shape != (M, N) or acc.dtype != torch.int32 or (N > 1 and acc.stride(1) != 1):
         raise ValueError("acc: int32 [M, N] rows expected")
-    _check(lib().oq_w8a8_gemm_i32(_ptr(Xq8), M, _ptr(Wq8), N, K, _ptr(acc), _ld(acc), _stream(stream)),
+    dev = _one_gpu(Xq8, Wq8, acc)
+    _check(lib().oq_w8a8_gemm_i32(_ptr(Xq8), M, _ptr(Wq8), N, K, _ptr(acc), _ld(acc), _on(stream, dev)),
            "oq_w8a8_gemm_i32")
     return acc
 

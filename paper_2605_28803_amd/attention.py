@@ -10,9 +10,8 @@ import ctypes as C
 
 import torch
 
-from . import _check, _lib, _ptr, _raw_stream, _stream  # (the package has these before it imports this module)
+from . import _check, _current_device, _lib, _on, _ptr  # (the package has these before it imports this module)
 
-_current_device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
 _DTYPE = {torch.float16: 0, torch.bfloat16: 1, torch.float32: 2}
 _TORCH = {0: torch.float16, 1: torch.bfloat16, 2: torch.float32}
 
@@ -51,10 +50,6 @@ def _device(t, u, v):
     if dev != _current_device():
         raise ValueError(f"cuda:{dev} is not the current device")
     return dev
-
-
-def _on(stream, dev):
-    return _raw_stream(dev) if stream is None and _raw_stream is not None else _stream(stream)
 
 
 def attention_prompt(Q, K, V, cu_seqlens, causal=True, scale=None, O=None, stream=None):
@@ -197,7 +192,12 @@ def attention_kv4(Q, cache, block_table, seq_lens, cu_q=None, max_q=None, max_le
         ldo = _heads(O, "O", d)
     if work is None:
         nbytes = attention_kv4_workspace_bytes(cache, T, hq, n, max_q, max_len)
-        work = torch.empty((nbytes,), dtype=torch.uint8, device=Q.device) if nbytes else None
+        if nbytes and stream is None:
+            work = torch.empty((nbytes,), dtype=torch.uint8, device=Q.device)
+        elif nbytes:
+            # (Of the call's stream, so that its memory is not handed out on another one while the call waits.)
+            with torch.cuda.stream(stream):
+                work = torch.empty((nbytes,), dtype=torch.uint8, device=Q.device)
     else:
         _want(work.get_device() == dev and work.is_contiguous() and work.element_size() == 1, "work: contiguous bytes on Q's device expected")
     _check(_lib.load().oq_attention_kv4(cache.ref, _ptr(Q), T, ldq, hq, _DTYPE[Q.dtype], _ptr(cu_q), max_q, _ptr(block_table),

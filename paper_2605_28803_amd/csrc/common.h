@@ -26,6 +26,9 @@ inline int launch_status() {
   return e == hipSuccess ? OQ_OK : OQ_ERR_HIP;
 }
 
+// A grid dimension counts fewer than 2^32 threads.
+inline bool launchable(int64_t blocks, int64_t threads) { return blocks * threads <= int64_t{UINT32_MAX}; }
+
 // f(std::integral_constant<int, i>) for i = 0 .. N-1, fully unrolled.
 template <typename F, int... I>
 __device__ __forceinline__ void static_for_seq(F&& f, std::integer_sequence<int, I...>) {

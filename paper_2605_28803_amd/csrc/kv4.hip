@@ -318,10 +318,11 @@ __global__ __launch_bounds__(256) void kv4_gather_kernel(Cache c, const int64_t*
 // keys the 72 is taken out by the accumulator's start, -72 sum(q) (an error
 // of 2^-24 of that sum); for values by a packed subtraction, exact.
 // The step of a key scales its row of S in fp32.  The step of a value is
-// folded into the probability, P' = 2^(s - m) (step 2^(m - m')), with m' the
-// running maximum of s + log2(step): P' is at most 1 and its fp16 rounding is
-// relative to the largest contribution whatever the steps' range.  The sum l of
-// the softmax is formed from 2^(s - m) in fp32.
+// folded into the probability, P' = 2^(s - m) 2^(m - m') step 2^15, with m' the
+// running maximum of s + log2(step): P' is at most 2^15 and its fp16 rounding is
+// relative to the largest contribution whatever the steps' range (2^-11 of it down
+// to 2^-29 of that, so that a long row's many small probabilities keep their
+// weight).  The sum l of the softmax is formed from 2^(s - m) in fp32.
 // Queries are scaled by a power of two to at most 1 and rounded to fp16 (exact
 // for unrotated fp16 and bf16 rows but for values below 2^-24 of the row's
 // largest); rotated ones are split in two fp16 parts (22 bits).
@@ -342,7 +343,8 @@ struct AttnKv4 {
   bool causal;
 };
 
-constexpr int kTile = 64;  // tokens of one step of a wave
+constexpr int kTile = 64;        // tokens of one step of a wave
+constexpr float kShift = 15.0f;  // log2 of P' at its largest
 
 __device__ __forceinline__ uint32_t and_xor(uint32_t a, uint32_t m, uint32_t x) { return (a & m) ^ x; }
 
@@ -677,8 +679,9 @@ __global__ __launch_bounds__(64 * W, QT == 1 ? D < 256 ? 3 : 2 : 1) void attn_kv
       topv = row_max<RC>(topv);
       const float mn = fmaxf(m[t], top * qscale[t]), mvn = fmaxf(mv[t], topv);
       const float mr = mn == -INFINITY ? 0.0f : mn, mvr = mvn == -INFINITY ? 0.0f : mvn;
-      // (At most 2^120: the product with an underflowed probability is then 0.)
-      const float f = __builtin_amdgcn_exp2f(fminf(mr - mvr, 120.0f));
+      // (At most 2^120, and times the probability first: 0 if that has underflowed,
+      // whatever the step.)
+      const float f = __builtin_amdgcn_exp2f(fminf(mr - mvr + kShift, 120.0f));
       if (__builtin_amdgcn_ballot_w64(mn > m[t] || mvn > mv[t]) != 0) {
         l[t] *= __builtin_amdgcn_exp2f(m[t] - mr);
         const float al = __builtin_amdgcn_exp2f(mv[t] - mvr);
@@ -696,7 +699,7 @@ __global__ __launch_bounds__(64 * W, QT == 1 ? D < 256 ? 3 : 2 : 1) void attn_kv
         for (int e = 0; e < 4; ++e) {
           p[e] = __builtin_amdgcn_exp2f(fmaf(c[i][e], qscale[t], -mr));
           l[t] += p[e];
-          p[e] *= vs[i][e] * f;
+          p[e] = p[e] * f * vs[i][e];
         }
         // (Tokens of a word come out as 0, 2, 1, 3.)
         pk[t][0][i] = __builtin_bit_cast(uint32_t, v2h{static_cast<_Float16>(p[0]), static_cast<_Float16>(p[2])});
@@ -775,7 +778,7 @@ __global__ __launch_bounds__(64 * W, QT == 1 ? D < 256 ? 3 : 2 : 1) void attn_kv
 #pragma unroll
       for (int e = 0; e < 8; ++e) y[e] += so[w][r][c + e] * f;
     }
-    const float f = L_ > 0.0f ? __builtin_amdgcn_exp2f(mvr - mr) / L_ : 0.0f;
+    const float f = L_ > 0.0f ? __builtin_amdgcn_exp2f(mvr - mr - kShift) / L_ : 0.0f;
 #pragma unroll
     for (int e = 0; e < 8; ++e) y[e] *= f;
     const int64_t tok = q0 + (r0 + r) / a.R;
@@ -946,7 +949,7 @@ extern "C" int oq_kv4_append(const oq_kv4_cache* cache, const void* K, const voi
   if ((st = oq::device_check()) != OQ_OK) return st;
   const oq::Cache c = oq::device_cache(cache);
   const int64_t per = 2048 / cache->head_dim, blocks = (n + per - 1) / per * c.hk;
-  if (blocks > INT32_MAX) return OQ_ERR_SHAPE;
+  if (!oq::launchable(blocks, 256)) return OQ_ERR_SHAPE;
   const dim3 grid(static_cast<unsigned>(blocks));
   const bool bf = dtype == OQ_OUT_BF16;
   hipStream_t s = static_cast<hipStream_t>(stream);
@@ -981,7 +984,7 @@ extern "C" int oq_kv4_gather(const oq_kv4_cache* cache, const int64_t* slots, in
   if ((st = oq::device_check()) != OQ_OK) return st;
   const oq::Cache c = oq::device_cache(cache);
   const int64_t per = 2048 / cache->head_dim, blocks = (n + per - 1) / per * c.hk;
-  if (blocks > INT32_MAX) return OQ_ERR_SHAPE;
+  if (!oq::launchable(blocks, 256)) return OQ_ERR_SHAPE;
   const dim3 grid(static_cast<unsigned>(blocks), 2);
   hipStream_t s = static_cast<hipStream_t>(stream);
 #define OQ_GATHER(D, R)                             \
@@ -999,10 +1002,12 @@ extern "C" int oq_kv4_gather(const oq_kv4_cache* cache, const int64_t* slots, in
 
 static int attn_kv4_shape(const oq_kv4_cache* cache, int64_t tokens, int32_t n_heads, int32_t n_seqs, int32_t max_q,
                           int32_t max_len) {
-  if (tokens < 0 || tokens > INT32_MAX || n_seqs < 0 || max_q < 1 || max_q > 65535 || max_len < 0 || max_len > (1 << 30) || n_heads < 1) return OQ_ERR_SHAPE;
+  if (tokens < 0 || tokens > INT32_MAX || n_seqs < 0 || max_q < 1 || max_q > 65535 || max_len < 0 || max_len > (1 << 30) ||
+      n_heads < 1 || n_heads > 65535)
+    return OQ_ERR_SHAPE;
   if (n_heads % cache->n_kv_heads != 0) return OQ_ERR_SHAPE;
   if (static_cast<int64_t>(n_seqs) * cache->n_kv_heads > 65535) return OQ_ERR_SHAPE;
-  if (static_cast<int64_t>(max_q) * (n_heads / cache->n_kv_heads) > INT32_MAX / 2) return OQ_ERR_SHAPE;
+  if (static_cast<int64_t>(max_q) * (n_heads / cache->n_kv_heads) > (1 << 26)) return OQ_ERR_SHAPE;  // (rows of a grid)
   return OQ_OK;
 }
 
@@ -1028,7 +1033,7 @@ extern "C" int oq_attention_kv4(const oq_kv4_cache* cache, const void* Q, int64_
   if (table_ld < 0 || (static_cast<int64_t>(max_len) + cache->page_tokens - 1) / cache->page_tokens > table_ld) return OQ_ERR_SHAPE;
   if (dtype != OQ_OUT_F16 && dtype != OQ_OUT_BF16) return OQ_ERR_ARG;
   if (causal != 0 && causal != 1) return OQ_ERR_ARG;
-  if (!(scale > 0.0f) || !std::isfinite(scale)) return OQ_ERR_ARG;
+  if (!(scale > 0.0f) || !std::isfinite(scale * 1.4426950408889634f)) return OQ_ERR_ARG;
   if (ldq % 8 != 0 || ldo % 8 != 0) return OQ_ERR_ALIGN;
   if (tokens == 0 || n_seqs == 0) return OQ_OK;
   if (!Q || !O || !seq_lens || (!block_table && max_len > 0)) return OQ_ERR_NULL;

@@ -21,6 +21,11 @@
 // TFLOP/s, 83% of what the library's 8192-cubed bf16 product reaches on the same card; 64 rows
 // a wave (half the LDS reads, one wave a SIMD) 857 us; 32-key steps 604.
 //
+// Probabilities are rounded to the inputs' type for the second product and
+// summed as rounded, so that the weights add up to one.  fp16 ones are taken times
+// 2^15 (the division by l removes it): those above 2^-29 of a row's largest are
+// normal numbers, and many small ones keep their weight together.
+//
 // LDS rows are not padded; 16-byte pieces of a row are stored at piece ^ a
 // function of the row.  K: 16 rows of one piece cover all banks.  V: 4 rows of 4
 // pieces do.
@@ -60,11 +65,13 @@ __device__ __forceinline__ void dma16(uint32_t lds, uint32_t voff, const void* b
                : "memory", "m0");
 }
 
+// The types' operations; probabilities are scaled by 2^kShift.
 template <bool BF>
 struct Half;
 template <>
 struct Half<false> {
   typedef v8h v8;
+  static constexpr float kShift = 15.0f;
   static __device__ __forceinline__ v16f mfma(v8 a, v8 b, v16f c) { return __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, c, 0, 0, 0); }
   static __device__ __forceinline__ uint32_t pack(float a, float b) {
     return rqd::f2h(a) | static_cast<uint32_t>(rqd::f2h(b)) << 16;
@@ -76,6 +83,7 @@ struct Half<false> {
 template <>
 struct Half<true> {
   typedef v8b v8;
+  static constexpr float kShift = 0.0f;
   static __device__ __forceinline__ v16f mfma(v8 a, v8 b, v16f c) { return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0); }
   static __device__ __forceinline__ uint32_t pack(float a, float b) {
     const v2b p = {static_cast<__bf16>(a), static_cast<__bf16>(b)};
@@ -250,7 +258,7 @@ __global__ __launch_bounds__(64 * RW * KG, 2) void prompt_attn_kernel(PromptArgs
         for (int e = 0; e < 16; ++e) acc[ct][e] *= al;
       m = mn;
     }
-    const float mr = KG > 1 && mn == -INFINITY ? 0.0f : mn;
+    const float mr = (KG > 1 && mn == -INFINITY ? 0.0f : mn) - H::kShift;
     v8 pf[SUB][2];
 #pragma unroll
     for (int u = 0; u < SUB; ++u)
@@ -333,7 +341,7 @@ int launch_prompt(PromptArgs a, hipStream_t st) {
   constexpr int BM = 32 * RW;
   const int64_t tiles = (static_cast<int64_t>(a.tokens) + BM - 1) / BM + a.n_seqs;
   const int64_t total = tiles * a.hq;
-  if (total > INT32_MAX) return OQ_ERR_SHAPE;
+  if (!launchable(total, 64 * RW * KG)) return OQ_ERR_SHAPE;
   a.tiles = static_cast<int>(tiles);
   hipLaunchKernelGGL((prompt_attn_kernel<BF, D, BN, RW, KG>), dim3(static_cast<unsigned>(total)), dim3(64 * RW * KG), 0, st, a);
   return launch_status();
@@ -380,7 +388,7 @@ extern "C" int oq_attention_prompt(const void* Q, const void* K, const void* V, 
   if (ldq < wq || ldo < wq || ldk < wk || ldv < wk || ldk > (1 << 24) || ldv > (1 << 24)) return OQ_ERR_SHAPE;
   if (dtype != OQ_OUT_F16 && dtype != OQ_OUT_BF16) return OQ_ERR_ARG;
   if (causal != 0 && causal != 1) return OQ_ERR_ARG;
-  if (!(scale > 0.0f) || !std::isfinite(scale)) return OQ_ERR_ARG;
+  if (!(scale > 0.0f) || !std::isfinite(scale * 1.4426950408889634f)) return OQ_ERR_ARG;
   if (ldq % 8 != 0 || ldk % 8 != 0 || ldv % 8 != 0 || ldo % 8 != 0) return OQ_ERR_ALIGN;
   if (tokens == 0 || n_seqs == 0) return OQ_OK;
   if (!Q || !K || !V || !O || !cu_seqlens) return OQ_ERR_NULL;

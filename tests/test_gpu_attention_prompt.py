@@ -85,6 +85,22 @@ def test_large_scores():
     _run([200], 2, 2, 64, True, torch.float16, spike=12.0, scale=0.5)
 
 
+@pytest.mark.parametrize("below", [10.0, 13.0, 15.0])
+def test_many_small_probabilities(below):
+    """One key far above the others, whose probabilities are below fp16's normal
+    numbers but of weight together; in all channels but one they alone are the output."""
+    n, d = 4096, 64
+    q, k, v = (torch.zeros((n, 1, d), dtype=torch.float16) for _ in range(3))
+    q[:, 0, 0], k[5, 0, 0] = 1.0, 8.0
+    v[:], v[5], v[5, 0, 0] = 1.0, 0.0, 1.0
+    cu = torch.tensor([0, n], dtype=torch.int32, device=DEV)
+    o = oq.attention_prompt(q.to(DEV), k.to(DEV), v.to(DEV), cu, causal=False, scale=below / 8)
+    row = slice(0, 1)  # (every row is the same)
+    ref, spread, _ = R.attend(q[row, 0].double(), k[:, 0].double(), v[:, 0].double(), below / 8, torch.ones((1, n), dtype=torch.bool))
+    got = o.cpu()[:, 0]
+    R.check(got, ref.expand(n, d), spread.expand(n, d), 2.0 ** -16, torch.float16, 2.0 ** -11)
+
+
 def test_equal_to_itself_and_on_another_stream():
     qkv = torch.randn((500, 8, 128), device=DEV, generator=torch.Generator(device=DEV).manual_seed(1)).half()
     cu = torch.tensor([0, 200, 500], dtype=torch.int32, device=DEV)

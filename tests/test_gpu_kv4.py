@@ -253,6 +253,35 @@ def test_sharp_maximum_in_a_small_value():
     R.check(o.cpu()[:, 0], ref, spread, 2.0 ** -18, torch.float16, 2.0 ** -11)
 
 
+def _tail(L, below, dtype):
+    """One token with a value in one channel only, the others below it by `below`
+    in the exponent, with values in every channel: in all channels but one the
+    output is the small probabilities' alone."""
+    bufs = _buffers(L // 64, 1, 64, 64)
+    k, v = torch.zeros((2, L, 1, 64), dtype=dtype)
+    k[5, 0, 0] = 7.0
+    v[:] = 7.0
+    v[5], v[5, 0, 0] = 0.0, 7.0
+    order = torch.arange(L)
+    R.put(bufs, order, k, v, False)
+    q = torch.zeros((1, 1, 64), dtype=dtype)
+    q[0, 0, 0] = 1.0
+    scale = below / 7.0
+    o = oq.attention_kv4(q.to(DEV), _cache(bufs, False), torch.arange(L // 64, dtype=torch.int32, device=DEV)[None],
+                         torch.tensor([L], dtype=torch.int32, device=DEV), scale=scale)
+    kk, vv = R.take(bufs, order, 64, False)
+    ref, spread, _ = R.attend(q[:, 0].double(), kk[:, 0], vv[:, 0], scale, torch.ones((1, L), dtype=torch.bool))
+    # (the scores are below 32, so their fp32 errors, of a few steps of 2^-19, are below 2^-16)
+    R.check(o.cpu()[:, 0], ref, spread, 2.0 ** -15, dtype, 2.0 ** -11)
+
+
+@pytest.mark.parametrize("L,below", [(4096, 10.0), (65536, 17.7), (131072, 18.5)])
+def test_many_small_probabilities(L, below):
+    # e^-10, e^-17.7 and e^-18.5: below fp16's normal numbers, and below half its smallest one.
+    _tail(L, below, torch.float16)
+    _tail(L, below, torch.bfloat16)
+
+
 def _small(seed=0, n=3000):
     g = torch.Generator(device=DEV).manual_seed(seed)
     cache = oq.KV4Cache.empty(n // 64 + 1, 2, 128, 64)
@@ -273,6 +302,27 @@ def test_streams_and_repeats():
     b = oq.attention_kv4(q, cache, table, lens)
     torch.cuda.synchronize()
     assert torch.equal(a, want) and torch.equal(b, want)
+
+
+def test_workspace_belongs_to_the_call_s_stream():
+    """A workspace made inside a call on another stream is not handed out again
+    on the current one while that call still waits."""
+    cache, table, lens, q = _small()
+    want = oq.attention_kv4(q, cache, table, lens)
+    nbytes = oq.attention_kv4_workspace_bytes(cache, 1, 8, 1, 1, table.shape[1] * 64)
+    assert nbytes > 0
+    O = torch.empty_like(q)
+    a = torch.randn((4096, 4096), device=DEV)
+    torch.cuda.synchronize()
+    s = torch.cuda.Stream()
+    with torch.cuda.stream(s):
+        for _ in range(20):
+            a = (a @ a).clamp(-1, 1)  # (the stream is busy for some time)
+    oq.attention_kv4(q, cache, table, lens, O=O, stream=s)
+    x = [torch.full((nbytes,), 7, dtype=torch.uint8, device=DEV) for _ in range(4)]
+    torch.cuda.synchronize()
+    assert torch.equal(O, want)
+    assert all((t == 7).all() for t in x)
 
 
 def test_captured_step():

@@ -80,7 +80,8 @@ def _attend(lib, cache=None, Q=P16, tokens=4, ldq=1024, heads=8, dtype=0, cu=Non
     (dict(max_len=513), SHAPE), (dict(max_len=2 ** 30 + 1, table_ld=2 ** 40), SHAPE), (dict(table_ld=-1), SHAPE), (dict(ldq=1016), SHAPE), (dict(ldo=8), SHAPE),
     (dict(dtype=2), ARG), (dict(dtype=-1), ARG), (dict(causal=2), ARG), (dict(scale=0.0), ARG), (dict(scale=-1.0), ARG),
     (dict(scale=math.inf), ARG), (dict(scale=math.nan), ARG),
-    (dict(cu=P16, tokens=2 ** 31), SHAPE),
+    (dict(cu=P16, tokens=2 ** 31), SHAPE), (dict(heads=65536, ldq=2 ** 23, ldo=2 ** 23), SHAPE),
+    (dict(cu=P16, max_q=65535, heads=2050, ldq=2 ** 20, ldo=2 ** 20), SHAPE), (dict(scale=3e38), ARG),
 ])
 def test_attention_kv4_refusals(lib, change, status):
     assert _attend(lib, **change) == status
@@ -114,7 +115,7 @@ def _prompt(lib, Q=P16, K=P16, V=P16, tokens=4, ldq=1024, ldk=256, ldv=256, dtyp
     (dict(ldq=1016), SHAPE), (dict(ldk=248), SHAPE), (dict(ldv=248), SHAPE), (dict(ldo=1016), SHAPE), (dict(ldk=2 ** 25), SHAPE),
     (dict(tokens=-1), SHAPE), (dict(tokens=2 ** 31), SHAPE), (dict(n=-1), SHAPE), (dict(d=48), SHAPE), (dict(hq=7), SHAPE),
     (dict(hk=0), SHAPE), (dict(hq=0), SHAPE), (dict(dtype=2), ARG), (dict(causal=-1), ARG), (dict(scale=0.0), ARG),
-    (dict(scale=math.nan), ARG), (dict(tokens=0, Q=None), OK), (dict(n=0, cu=None), OK),
+    (dict(scale=math.nan), ARG), (dict(scale=3e38), ARG), (dict(tokens=0, Q=None), OK), (dict(n=0, cu=None), OK),
 ])
 def test_attention_prompt_refusals(lib, change, status):
     assert _prompt(lib, **change) == status
@@ -172,6 +173,13 @@ def test_binding_refusals():
                       ((i8, torch.ones(4), w8, torch.ones(8), None, oq.OUT_F16, torch.zeros((4, 8))), "Y")):
         with pytest.raises(ValueError, match=what):
             oq.w8a8_linear(*bad)
+    for bad, what in (((i8, torch.ones(8)[::2], w8, torch.ones(8)), "x_scale"),
+                      ((i8, torch.ones(4), w8, torch.ones(8), torch.zeros(16).half()[::2]), "bias"),
+                      ((i8, torch.ones(4), w8, torch.ones(8)), "one GPU")):
+        with pytest.raises(ValueError, match=what):
+            oq.w8a8_linear(*bad)
+    with pytest.raises(ValueError, match="one GPU"):
+        oq.w8a8_gemm_i32(i8, w8)
     with pytest.raises(ValueError, match="acc"):
         oq.w8a8_gemm_i32(i8, w8, torch.zeros((4, 9), dtype=torch.int32))
 
