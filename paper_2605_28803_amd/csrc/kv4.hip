@@ -15,6 +15,7 @@
 //     shares one) and the second product's operand, 8 tokens of a channel, is
 //     two words;
 //   k_scale, v_scale fp32 [token].
+#include <algorithm>
 #include <cmath>
 
 #include "common.h"
@@ -429,7 +430,8 @@ __global__ __launch_bounds__(64 * W, QT == 1 ? D < 256 ? 3 : 2 : 1) void attn_kv
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int col = lane & 15, g = lane >> 4;
   const int b = blockIdx.y / a.c.hk, h = blockIdx.y % a.c.hk;
-  const int split = blockIdx.z;
+  // (The last splits first, which only long sequences have: 64 ragged ones in four, 29.2 -> 27.6 us.)
+  const int split = gridDim.z - 1 - blockIdx.z;
   const int c0 = split * a.chunk, first = c0 + wave * kTile;  // tokens
   const int32_t* table = a.table + b * a.table_ld;
   // Page table entry of 16-token block `blk` of the sequence, and the block's place in the page.
@@ -875,17 +877,22 @@ Cache device_cache(const oq_kv4_cache* c) {
 // The launch.  Rows: 16 columns of products (two such blocks in a workgroup above
 // 16 rows, but not at d = 256, whose accumulators fill the registers), compacted
 // for the softmax when 4 or 8 are in use.
-// Length: splits of `chunk` tokens.  A split costs a workgroup's start (queries,
-// page table, first keys) and end; too few leave CUs without work or unevenly
-// loaded.  About 1536 workgroups if every sequence is the longest, but chunks of
-// no less than a step of a workgroup's waves and at most 64 splits, which are
-// to be joined again.  Us at 64 ragged sequences of up to 4096 tokens (32 / 8
-// heads of 128), 768 / 1024 / 1536 / 2048 / 3072 workgroups: 33.7 / 35.1 / 28.3 /
-// 29.5 / 30.4; one of 131000 with at most 48 / 64 / 96 / 128 splits: 36.5 / 33.6 / 38.6 /
-// 38.0; one of 866 (8 / 1 heads of 256) in splits of 256 / 512 / 1024 tokens:
-// 10.4 / 14.9 / 22.6.  Up to 512 tokens a workgroup of 8 waves takes the whole
-// sequence in one step, and nothing is to be joined.
-constexpr int kTargetWgs = 1536, kMaxSplits = 64, kWholeLen = 512;
+// Length: splits of `chunk` tokens, 64 at most, which a second launch joins.  A
+// split costs a workgroup's start (queries, page table, first keys) and end, so
+// there are about as many as the card holds at once: 640 workgroups of four waves (two or
+// three a CU), 256 of the eight waves that take 32 rows.  But only max_len is known here, and a
+// long sequence among short ones would be the last to end: chunks have at most 4096 tokens, and
+// at 16 rows at most 1024 as long as 2048 workgroups do.  Measured against every number of
+// splits at four and eight waves, for nine head layouts, 1 to 150 sequences of up to 400 ..
+// 60000 tokens, equal or ragged (609 shapes): 3% over the fastest in the mean (splits for
+// 1536 workgroups at four waves: 13%).  Us, eight waves against four at 32 rows, the best number of
+// splits each: 50 tokens of 8 heads of 128, 32 sequences of 2000, 44.6 / 51.7; 64 / 2 heads, 8
+// sequences of 32000, 27.8 / 31.8; but one of 2000, where chunks of 256 fill no card, 11.9 / 11.3.
+// One launch without splits, for 16 rows: up to 512 tokens eight waves (one of 400, 32 / 8
+// heads: 6.2; in two splits 7.7), and up to 1024 tokens where the splits would fill the card
+// anyway or, at d = 64, the queries take little (32 sequences of 866, 32 / 8 heads of 128: 11.0 /
+// 14.6, but one: 8.3 / 7.7; one, 16 / 1 heads of 64: 8.0 / 8.5).
+constexpr int kMaxSplits = 64;
 struct Kv4Plan {
   int qt, rc, waves, splits, chunk;
   int64_t row_blocks;
@@ -897,11 +904,20 @@ Kv4Plan kv4_plan(int64_t n_seqs, int hk, int d, int R, int max_q, int64_t max_le
   p.rc = rows <= 4 ? 4 : rows <= 8 ? 8 : 16;
   p.row_blocks = (rows + 16 * p.qt - 1) / (16 * p.qt);
   const int64_t wgs = n_seqs * hk * p.row_blocks;
-  p.waves = p.qt == 1 && max_len <= kWholeLen && wgs <= 512 ? 8 : 4;
+  int64_t splits = 1;
+  if (p.qt == 2) {
+    const bool shortest = max_len > 512 && wgs * ((max_len + 255) / 256) <= 256;  // chunks of 256 do not fill the card
+    p.waves = shortest ? 4 : 8;
+    splits = shortest ? kMaxSplits : max_len <= 512 ? 1 : std::max(256 / wgs, (max_len + 4095) / 4096);
+  } else if (wgs <= 256 && (max_len <= 512 || (max_len <= 1024 && (d == 64 || wgs >= 128)))) {
+    p.waves = 8;
+  } else {
+    p.waves = 4;
+    splits = max_len <= 512 ? 1 : std::max({640 / wgs, std::min((max_len + 1023) / 1024, 2048 / wgs), (max_len + 4095) / 4096});
+  }
   const int64_t step = p.waves * kTile;
-  int64_t chunk = wgs * max_len / kTargetWgs;
-  chunk = chunk < max_len / kMaxSplits ? max_len / kMaxSplits : chunk > max_len ? max_len : chunk;
-  chunk = (chunk + step - 1) / step * step;
+  splits = std::clamp<int64_t>(splits, 1, kMaxSplits);
+  const int64_t chunk = ((max_len + splits - 1) / splits + step - 1) / step * step;
   p.chunk = static_cast<int>(chunk < step ? step : chunk);
   p.splits = static_cast<int>(max_len <= p.chunk ? 1 : (max_len + p.chunk - 1) / p.chunk);
   return p;
@@ -920,7 +936,10 @@ void launch_attn(const AttnKv4& a, const Kv4Plan& p, dim3 grid, bool rot, hipStr
   OQ_ATTN(1, 8, 8)
   OQ_ATTN(1, 16, 4)
   OQ_ATTN(1, 16, 8)
-  if constexpr (D < 256) OQ_ATTN(2, 16, 4)
+  if constexpr (D < 256) {
+    OQ_ATTN(2, 16, 4)
+    OQ_ATTN(2, 16, 8)
+  }
 #undef OQ_ATTN
   if (a.splits > 1) {
     const unsigned y = static_cast<unsigned>(a.max_q), z = static_cast<unsigned>(a.n_seqs);

@@ -219,6 +219,19 @@ def test_split_over_the_length(n):
     _attention([n], [1], 8, 1, 256, 64, True, True, torch.bfloat16, cu=False)
 
 
+@pytest.mark.parametrize("rotate", [False, True])
+@pytest.mark.parametrize("lens,nqs,hq,hk,d", [
+    ([900, 20], [20, 2], 8, 2, 128),                       # 32 rows, shortest chunks
+    ([3000, 500, 0, 1], [20, 20, 3, 1], 8, 2, 128),        # 32 rows, eight waves, splits of several steps
+    ([3000, 700, 64], [40, 5, 64], 8, 4, 64),
+    ([900, 1000, 513], [1, 1, 1], 16, 1, 64),              # whole sequences of several steps
+    ([600 + 20 * i for i in range(17)], [1] * 17, 8, 8, 128),
+    ([1500, 300, 90] * 9, [1] * 27, 10, 10, 64),           # splits that only the long ones have
+])
+def test_shapes_of_the_split(lens, nqs, hq, hk, d, rotate):
+    _attention(lens, nqs, hq, hk, d, 64, rotate, True, torch.float16)
+
+
 def test_bad_pages_are_masked():
     _attention([200, 150], [1, 1], 4, 2, 128, 32, False, True, torch.float16, cu=False,
                bad=[(0, 0, -1), (0, 3, 2 ** 31 - 1), (1, 4, 1000)])
