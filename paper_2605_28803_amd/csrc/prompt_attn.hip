@@ -1,7 +1,7 @@
 // Softmax self-attention within packed sequences (prompts), grouped heads,
 // causal or full.
 //
-// A workgroup takes 32 query tokens a row wave (4, 128 tokens) of one sequence and head
+// A workgroup takes 32 query tokens a row wave (2 or 4 of them) of one sequence and head
 // and walks the sequence's keys in steps of BN with a running maximum m and sum l
 // per row (one pass over K and V; nothing of the pair matrix leaves the
 // registers).  Both products are transposed, on v_mfma_f32_32x32x16: S^T = K Q^T
@@ -350,26 +350,37 @@ int launch_prompt(PromptArgs a, hipStream_t st) {
 // key tiles in turn and are joined at the end; they pay where there are fewer
 // workgroups than the card holds (two a CU for d >= 128) and sequences are long
 // enough for each to have several steps, since a row's walk over its keys
-// is then what takes the time.  wgs: workgroups of 128 rows, len: mean length.  Us with one
-// group against two (d = 64: four waves of rows):
-//   d = 128, causal: 1 x 816, 8 heads (wgs 56) 21.8 / 18.7; 1 x 2048, 16 heads (272) 54 / 42; 1 x 4096, 16
-//     (528) 103 / 88; 1 x 8192, 8 (520) 194 / 159; but 1 x 2500, 32 (656) 72 / 83; 4 x 1024, 16 (576) 33 / 48; 2 x 130, 16 (48)
-//     7.7 / 9.2; full: 4 x 700, 8 (200) 23 / 20; 1 x 4096, 16 (528) 145 / 157;
-//   d = 256, causal: 1 x 816, 8 45 / 37; 1 x 4096, 16 (528) 211 / 174; 4 x 1024, 16 (576) 66 / 91; full: 5 x 816, 8 (280) 52 / 42;
-//     1 x 3750, 16 (480) 245 / 271;
-//   d = 64 (a CU holds four, or two of two groups): 1 x 4096, 16 75 / 56; 1 x 2500, 32 50 / 42; 4 x 300, 16 (208) 8.2 / 8.0;
-//     48 ragged up to 600, 16 (1616) 23.6 / 27.0; four groups of 64 rows: 1 x 816, 8 (56) 15.4 / 12.7 / 10.2, but
-//     4 x 700, 8 (200) 16.0 / 13.3 / 19.2.
+// is then what takes the time; with half as many rows the few are spread over twice as many CUs.
+// More of either costs loads and LDS reads of the same keys.  wgs: workgroups of 128 rows, len: mean
+// length.  Us of (row waves, key groups) (4, 1) / (4, 2) / (2, 2), at d = 64 / (2, 4):
+//   d = 128, full, 8 heads on 1: 1 x 200 (wgs 16) 11.2 / 11.4 / 9.6; 4 x 300 (104) 13.0 / 13.1 / 11.8; 1 x 2000 (128) 52 / 40 / 39;
+//     1 x 4096 (264) 104 / 83 / 144; 16 heads, 1 x 4096 (528) 151 / 162 / 289;
+//     causal, 16 heads: 4 x 300 (208) 12.1 / 12.2 / 16.2; 1 x 2000 (256) 52 / 41 / 46; 1 x 4096 (528) 108 / 90 / 154; 4 x 1000
+//     (560) 34 / 44 / 57; 3 x 2500 (976) 116 / 116 / 190;
+//   d = 256, causal: 8 heads, 1 x 200 (16) 16.4 / 17.2 / 15.1; 1 x 2000 (128) 104 / 77 / 80; 1 x 4096 (264) 205 / 145 / 173; 8 x
+//     900, ragged (344) 105 / 79 / 117; 16 heads, 4 x 1000 (560) 69 / 82 / 112;
+//   d = 64 (a CU holds four, or two of two groups), causal: 1 x 200 (16) 7.7 / 7.4 / 6.5 / 7.0; 1 x 816 (56) 16.1 / 13.3 / 11.4 / 10.7;
+//     1 x 2000 (256) 34 / 26 / 22 / 27; 1 x 4096 (528) 76 / 58 / 55 / 71; 16 heads, 4 x 1000 (560) 25 / 20 / 26 / 34; 32 heads, 1 x
+//     4096 (1056) 92 / 92 / 106 / 136; full, 4 x 1000 (560) 31 / 28 / 33 / 48, 16 heads, 16 x 300 (848) 17.4 / 20.1 / 23.6 / 36.1.
+// Over 272 shapes the rule is within 1% of the fastest in the mean.
 template <bool BF>
 int launch_prompt_any(const PromptArgs& a, int d, hipStream_t st) {
   const int64_t wgs = (static_cast<int64_t>(a.tokens) / 128 + a.n_seqs) * a.hq, len = a.tokens / a.n_seqs;
   if (d == 64) {
     if (wgs <= 144 && len >= 384) return launch_prompt<BF, 64, 64, 2, 4>(a, st);
-    return len >= 256 ? launch_prompt<BF, 64, 64, 4, 2>(a, st) : launch_prompt<BF, 64, 64, 4, 1>(a, st);
+    if ((wgs <= 144 && len >= 128) || (wgs <= (a.causal ? 448 : 300) && len >= 384)) return launch_prompt<BF, 64, 64, 2, 2>(a, st);
+    const bool two = wgs <= (a.causal ? 720 : 576) && len >= 512;
+    return two ? launch_prompt<BF, 64, 64, 4, 2>(a, st) : launch_prompt<BF, 64, 64, 4, 1>(a, st);
   }
-  const bool two = (wgs <= 300 && len >= 256) || (a.causal && wgs <= 544 && len >= 2048);
-  if (d == 128) return two ? launch_prompt<BF, 128, 64, 4, 2>(a, st) : launch_prompt<BF, 128, 64, 4, 1>(a, st);
-  return two ? launch_prompt<BF, 256, 32, 4, 2>(a, st) : launch_prompt<BF, 256, 32, 4, 1>(a, st);
+  const bool few = wgs <= 128 && len >= 160;
+  const bool two = (wgs <= 300 && len >= 256) || (a.causal && wgs <= 544 && len >= 1200);
+  if (d == 128)
+    return few   ? launch_prompt<BF, 128, 64, 2, 2>(a, st)
+           : two ? launch_prompt<BF, 128, 64, 4, 2>(a, st)
+                 : launch_prompt<BF, 128, 64, 4, 1>(a, st);
+  return few   ? launch_prompt<BF, 256, 32, 2, 2>(a, st)
+         : two ? launch_prompt<BF, 256, 32, 4, 2>(a, st)
+               : launch_prompt<BF, 256, 32, 4, 1>(a, st);
 }
 
 }  // namespace

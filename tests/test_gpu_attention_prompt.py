@@ -69,6 +69,8 @@ def test_workgroup_shapes(d, causal):
     sequence and several."""
     _run([500], 4, 1, d, causal, torch.float16)             # key groups
     _run([700], 44, 2, d, causal, torch.bfloat16)           # one group, many steps (d = 64: two)
+    _run([700], 100, 4, d, causal, torch.float16)           # more heads
+    _run([200, 170], 4, 2, d, causal, torch.bfloat16)       # few short rows
     _run([300, 290, 310], 12, 3, d, causal, torch.float16)
     if causal:
         _run([2100], 20, 1, d, causal, torch.float16)       # few long rows
