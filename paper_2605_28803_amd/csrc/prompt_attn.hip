@@ -357,8 +357,8 @@ int launch_prompt(PromptArgs a, hipStream_t st) {
 //     1 x 4096 (264) 104 / 83 / 144; 16 heads, 1 x 4096 (528) 151 / 162 / 289;
 //     causal, 16 heads: 4 x 300 (208) 12.1 / 12.2 / 16.2; 1 x 2000 (256) 52 / 41 / 46; 1 x 4096 (528) 108 / 90 / 154; 4 x 1000
 //     (560) 34 / 44 / 57; 3 x 2500 (976) 116 / 116 / 190;
-//   d = 256, causal: 8 heads, 1 x 200 (16) 16.4 / 17.2 / 15.1; 1 x 2000 (128) 104 / 77 / 80; 1 x 4096 (264) 205 / 145 / 173; 8 x
-//     900, ragged (344) 105 / 79 / 117; 16 heads, 4 x 1000 (560) 69 / 82 / 112;
+//   d = 256, causal: 8 heads, 1 x 200 (16) 16.4 / 17.2 / 15.1; 1 x 2000 (128) 104 / 77 / 80; 1 x 4096 (264) 205 / 145 / 173; 4 x
+//     2000, ragged (344) 105 / 79 / 117; 16 heads, 4 x 1000 (560) 69 / 82 / 112;
 //   d = 64 (a CU holds four, or two of two groups), causal: 1 x 200 (16) 7.7 / 7.4 / 6.5 / 7.0; 1 x 816 (56) 16.1 / 13.3 / 11.4 / 10.7;
 //     1 x 2000 (256) 34 / 26 / 22 / 27; 1 x 4096 (528) 76 / 58 / 55 / 71; 16 heads, 4 x 1000 (560) 25 / 20 / 26 / 34; 32 heads, 1 x
 //     4096 (1056) 92 / 92 / 106 / 136; full, 4 x 1000 (560) 31 / 28 / 33 / 48, 16 heads, 16 x 300 (848) 17.4 / 20.1 / 23.6 / 36.1.
