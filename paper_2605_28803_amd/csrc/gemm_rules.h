@@ -131,11 +131,22 @@ constexpr int ring_tiling(int64_t M, int64_t N, int64_t K, bool a8) {
 
 // W8A8: whether the small-M kernel takes a product; the ring's 64 x 64 tiles with
 // three buffers are faster from there on.  Weights from HBM, us on the small-M
-// kernel against the ring: 1 x 2560 x 2048 5.4 / 7.4, 16 x 2048 x 8192 10.6 / 16.9, 16 x 5000 x
-// 8192 14.5 / 17.4, 16 x 32768 x 2048 17.0 / 16.8 (at worst 16 x 8200 x 4096 12.4 / 11.4); 17 x 8200
+// kernel against the ring: 1 x 2560 x 2048 5.4 / 7.4, 16 x 2048 x 8192 10.5 / 16.9, 16 x 5000 x
+// 8192 14.8 / 17.4, 16 x 32768 x 2048 16.6 / 16.8 (at worst 16 x 8200 x 4096 12.3 / 11.4); 17 x 8200
 // x 4096 13.5 / 11.3; 17 x 2048 x 16384 19.8 / 29.3, 32 x 2048 x 16384 24.6 / 29.3 (two row blocks a workgroup;
 // with four, of which two are empty, 28.3), 40 x 4096 x 4096 10.9 / 10.8.
 constexpr bool w8_few_rows(int64_t M, int64_t N) { return M <= 16 || (M <= 32 && N <= 4096); }
+
+// Its shape there (as small_shape): eight waves and one unit a round, so that two or three
+// workgroups a CU overlap each other's waits, but rows of more than 8192 codes, whose walk is
+// long, four units (1 x 2560 x 16384: 12.4 us, one unit 13.9).  Us of 16 waves, as W4A4, against eight: 16 x 4096 x
+// 16384 20.5 / 19.4, 16 x 5000 x 8192 15.2 / 14.8; of two units against one at 32 columns: 16 x 32768 x 8192 62 / 53.4, 16
+// x 6144 x 8192 17.9 / 17.2, 8 x 16384 x 4096 18.1 / 17.7.
+constexpr SmallShape w8_small_shape(int64_t N, int64_t K) {
+  if (N > 4096) return {2, 8, K < 128 ? 0 : 1};
+  if (K <= 1024) return {1, 4, K < 128 ? 0 : 2};
+  return {1, 8, K <= 8192 ? 1 : 4};
+}
 
 // W8A8 tilings (both operands staged as they are, 128-code stages): 256 x 256 and
 // 128 x 128 of 8 waves, 128 x 64 and 64 x 64 of 4 (the last with three

@@ -284,7 +284,7 @@ __global__ __launch_bounds__(64 * WAVES) void gemm_small_kernel(GemmArgs a) {
 
 template <int EPI, bool TILED, int MB, bool A8 = false, bool W8 = false>
 int launch_small_mb(const GemmArgs& a, hipStream_t stream) {
-  const SmallShape sh = small_shape(a.N, a.K, A8);
+  const SmallShape sh = W8 ? w8_small_shape(a.N, a.K) : small_shape(a.N, a.K, A8);
   const int bn = 16 * sh.nb;
   const dim3 grid(static_cast<unsigned>((a.N + bn - 1) / bn), static_cast<unsigned>((a.M + 16 * MB - 1) / (16 * MB)));
   const dim3 block(64 * sh.waves);
@@ -299,8 +299,13 @@ int launch_small_mb(const GemmArgs& a, hipStream_t stream) {
   }
   OQ_SMALL(1, 4, 2)
   OQ_SMALL(2, 8, 1)
-  OQ_SMALL(1, 16, 1)
-  OQ_SMALL(2, 8, 2)
+  if constexpr (W8) {
+    OQ_SMALL(1, 8, 1)
+    OQ_SMALL(1, 8, 4)
+  } else {
+    OQ_SMALL(1, 16, 1)
+    OQ_SMALL(2, 8, 2)
+  }
   if constexpr (!A8) {
     OQ_SMALL(1, 16, 2)
     OQ_SMALL(2, 8, 4)

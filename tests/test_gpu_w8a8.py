@@ -16,6 +16,7 @@ CASES = [
     (64, 520, 4160), (3, 100, 64), (65, 320, 1536), (130, 1000, 1024), (256, 4096, 4096), (1000, 2048, 2112), (50, 1024, 4096),
     (700, 4104, 192), (129, 257, 320), (2000, 2056, 704), (300, 8200, 64), (64, 20000, 128), (5, 33000, 1088), (20, 520, 4160),
     (1000, 4096, 320), (3000, 3000, 1024), (4100, 4096, 1024), (4096, 4104, 1024),
+    (2, 300, 16384), (30, 4096, 8256), (16, 4104, 4160), (13, 6000, 16384), (1, 5000, 64), (27, 1000, 1088), (9, 5000, 2176),
 ]
 
 
