@@ -301,8 +301,14 @@ def quantize_weights_i8(W_u, had_block, Wq8=None, w_scale=None, stream=None):
         Wq8 = torch.empty((N, K), dtype=torch.int8, device=W_u.device)
     if w_scale is None:
         w_scale = torch.empty((N,), dtype=torch.float32, device=W_u.device)
+    if W_u.dtype != torch.float16 or (K > 1 and W_u.stride(1) != 1):
+        raise ValueError("W_u: float16 [N, K] rows expected")
+    if (Wq8.shape != (N, K) or Wq8.dtype != torch.int8 or not Wq8.is_contiguous() or w_scale.shape != (N,)
+            or w_scale.dtype != torch.float32 or not w_scale.is_contiguous()):
+        raise ValueError("Wq8 and w_scale: contiguous int8 [N, K] and float32 [N] expected")
+    dev = _one_gpu(W_u, Wq8, w_scale)
     _check(lib().oq_quantize_weights_i8(_ptr(W_u), N, K, _ld(W_u), had_block, _ptr(Wq8), _ptr(w_scale),
-                                        _stream(stream)), "oq_quantize_weights_i8")
+                                        _on(stream, dev)), "oq_quantize_weights_i8")
     return Wq8, w_scale
 
 
@@ -335,7 +341,7 @@ def w8a8_linear(Xq8, x_scale, Wq8, w_scale, bias=None, out_dtype=OUT_F16, Y=None
         raise ValueError("bias: contiguous float16 [N] expected")
     dt = torch.float16 if out_dtype == OUT_F16 else torch.bfloat16
     if Y is None:
-        Y = torch.empty((M, N), dtype=dt, device=Xq8.device)
+        Y = Xq8.new_empty((M, N), dtype=dt)
     elif Y.shape != (M, N) or Y.dtype != dt or (N > 1 and Y.stride(1) != 1):
         raise ValueError("Y: [M, N] rows of out_dtype expected")
     dev = _one_gpu(Xq8, x_scale, Wq8, w_scale, Y) if bias is None else _one_gpu(Xq8, x_scale, Wq8, w_scale, Y, bias)

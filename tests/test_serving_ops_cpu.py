@@ -180,6 +180,10 @@ def test_binding_refusals():
             oq.w8a8_linear(*bad)
     with pytest.raises(ValueError, match="one GPU"):
         oq.w8a8_gemm_i32(i8, w8)
+    for bad, what in (((h(8, 64).float(), 64), "W_u"), ((h(64, 8).t(), 64), "W_u"), ((h(8, 64), 64, w8[:4]), "Wq8"),
+                      ((h(8, 64), 64, w8, torch.ones(4)), "w_scale"), ((h(8, 64), 64, w8, torch.ones(8)), "one GPU")):
+        with pytest.raises(ValueError, match=what):
+            oq.quantize_weights_i8(*bad)
     with pytest.raises(ValueError, match="acc"):
         oq.w8a8_gemm_i32(i8, w8, torch.zeros((4, 9), dtype=torch.int32))
 
