@@ -17,9 +17,9 @@
 // cycles of matrix instructions, about 700 of the vector unit (32 exponentials at a
 // quarter of its rate, as many multiply-adds, half as many maxima, packed roundings and dot
 // products that add the rounded probabilities) and 32 KB of LDS reads; two waves a SIMD
-// overlap them.  One causal sequence of 8192, 32 / 8 heads of 128: 561 us, 980
-// TFLOP/s, 83% of what the library's 8192-cubed bf16 product reaches on the same card; 64 rows
-// a wave (half the LDS reads, one wave a SIMD) 857 us; 32-key steps 604.
+// overlap them.  One causal sequence of 8192, 32 / 8 heads of 128: 544 us, 1010
+// TFLOP/s, 85% of what the library's 8192-cubed bf16 product reaches on the same card; 64 rows
+// a wave (half the LDS reads, one wave a SIMD) 857 against 561 us; 32-key steps 604.
 //
 // Probabilities are rounded to the inputs' type for the second product and
 // summed as rounded, so that the weights add up to one.  fp16 ones are taken times
@@ -275,6 +275,9 @@ __global__ __launch_bounds__(64 * RW * KG, 2) void prompt_attn_kernel(PromptArgs
         }
         pf[u][j] = __builtin_bit_cast(v8, pk);
       }
+    // The second product goes before another wave's softmax (1 x 4096, 16 full heads of 128: 143 -> 135 us;
+    // of 256 269 -> 264; at d = 64, and at 128 with key groups, in step at their barrier, up to 1% slower).
+    if constexpr (D == 256 || (KG == 1 && D == 128)) __builtin_amdgcn_s_setprio(1);
 #pragma unroll
     for (int ct = 0; ct < CT; ++ct)
 #pragma unroll
@@ -292,6 +295,7 @@ __global__ __launch_bounds__(64 * RW * KG, 2) void prompt_attn_kernel(PromptArgs
                     sb + voff[ct % VO] + (ct / VO) * (64 * VO) + (32 * u + 16 * j + 8 * y) * ROWB))));
           acc[ct] = H::mfma(vf.o, pf[u][j], acc[ct]);
         }
+    if constexpr (D == 256 || (KG == 1 && D == 128)) __builtin_amdgcn_s_setprio(0);
   }
   l += rqd::lane_xor_far<32>(l);
   if constexpr (KG > 1) {
