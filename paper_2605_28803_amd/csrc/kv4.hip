@@ -780,7 +780,8 @@ __global__ __launch_bounds__(64 * W, QT == 1 ? D < 256 ? 3 : 2 : 1) void attn_kv
 #pragma unroll
       for (int e = 0; e < 8; ++e) y[e] += so[w][r][c + e] * f;
     }
-    const float f = L_ > 0.0f ? __builtin_amdgcn_exp2f(mvr - mr - kShift) / L_ : 0.0f;
+    // (No value maximum: every value that the row sees has step 0.)
+    const float f = L_ > 0.0f && MV > -INFINITY ? __builtin_amdgcn_exp2f(mvr - mr - kShift) / L_ : 0.0f;
 #pragma unroll
     for (int e = 0; e < 8; ++e) y[e] *= f;
     const int64_t tok = q0 + (r0 + r) / a.R;

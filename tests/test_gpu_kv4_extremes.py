@@ -1,0 +1,61 @@
+"""Attention over the 4-bit cache where its numbers are extreme: rows of zero
+values under strongly negative scores.  All expected values are float64's."""
+import pytest
+import torch
+
+import paper_2605_28803_amd as oq
+from tests import serving_ref as R
+
+pytestmark = pytest.mark.gpu
+DEV = torch.device("cuda:0")
+
+
+def _call(q, k, v, scale, rotate=False, page=64, causal=True):
+    """q [nq, hq, d] over one sequence k, v [L, hk, d]: (output, the cache's keys and values as float64)."""
+    L, hk, d = k.shape
+    pages = -(-L // page)
+    bufs = [torch.zeros((pages, hk, page, d // 2), dtype=torch.uint8),
+            torch.zeros((pages, hk, page // 16, d // 2, 16), dtype=torch.uint8),
+            torch.full((pages, hk, page), float("nan")), torch.full((pages, hk, page), float("nan"))]
+    order = torch.arange(L)
+    R.put(bufs, order, k, v, rotate)
+    cache = oq.KV4Cache(*(b.to(DEV) for b in bufs), rotate_k=rotate)
+    cu = None if q.shape[0] == 1 else torch.tensor([0, q.shape[0]], dtype=torch.int32, device=DEV)
+    o = oq.attention_kv4(q.to(DEV), cache, torch.arange(pages, dtype=torch.int32, device=DEV)[None],
+                         torch.tensor([L], dtype=torch.int32, device=DEV), cu, max_q=q.shape[0], max_len=L, causal=causal,
+                         scale=scale)
+    torch.cuda.synchronize()
+    return o.cpu(), *R.take(bufs, order, d, rotate)
+
+
+@pytest.mark.parametrize("dtype", [torch.float16, torch.bfloat16])
+@pytest.mark.parametrize("d,rotate", [(64, False), (128, True), (256, False)])
+@pytest.mark.parametrize("below", [90.0, 100.0, 150.0, 1000.0])
+@pytest.mark.parametrize("L", [1, 64, 700, 6000])
+def test_zero_values_under_low_scores(L, below, d, rotate, dtype):
+    """Every score is -below and every value 0: the output is 0, exactly."""
+    q, k = torch.zeros((1, 4, d), dtype=dtype), torch.zeros((L, 2, d), dtype=dtype)
+    q[:, :, 0], k[:, :, 0] = 1.0, -1.0
+    o, _, _ = _call(q, k, torch.zeros_like(k), below, rotate)
+    assert (o == 0).all()
+
+
+@pytest.mark.parametrize("dtype", [torch.float16, torch.bfloat16])
+@pytest.mark.parametrize("nq", [1, 3, 10])
+@pytest.mark.parametrize("L,start,stop", [(128, 0, 64), (700, 64, 600), (6000, 0, 2500), (6000, 2000, 5990)])
+def test_zero_values_beside_others(L, start, stop, nq, dtype):
+    """A run of tokens with zero values and scores of -below, between tokens of
+    score 0: it weighs nothing, in whatever wave or split it lies."""
+    d = 128
+    g = torch.Generator().manual_seed(L + nq)
+    for below in (95.0, 110.0, 400.0):
+        q, k = torch.zeros((nq, 4, d), dtype=dtype), torch.zeros((L, 2, d), dtype=dtype)
+        v = torch.randn((L, 2, d), generator=g).to(dtype)
+        q[:, :, 0] = 1.0
+        k[start:stop, :, 0], v[start:stop] = -1.0, 0.0
+        o, kk, vv = _call(q, k, v, below)
+        see = torch.arange(L)[None, :] <= (L - nq + torch.arange(nq))[:, None]
+        for h in range(4):
+            ref, spread, _ = R.attend(q[:, h].double(), kk[:, h // 2], vv[:, h // 2], below, see)
+            # (The other tokens' keys have step 0: their scores are 0 exactly.)
+            R.check(o[:, h], ref, spread, 2.0 ** -18, dtype, 2.0 ** -11)
