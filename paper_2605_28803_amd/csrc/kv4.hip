@@ -319,11 +319,12 @@ __global__ __launch_bounds__(256) void kv4_gather_kernel(Cache c, const int64_t*
 // keys the 72 is taken out by the accumulator's start, -72 sum(q) (an error
 // of 2^-24 of that sum); for values by a packed subtraction, exact.
 // The step of a key scales its row of S in fp32.  The step of a value is
-// folded into the probability, P' = 2^(s - m) 2^(m - m') step 2^15, with m' the
-// running maximum of s + log2(step): P' is at most 2^15 and its fp16 rounding is
+// folded into the probability, P' = 2^(s - m) step 2^E with E = min(15 - m', 126) and m' the
+// running maximum of s - m + log2(step): P' is at most 2^15 and its fp16 rounding is
 // relative to the largest contribution whatever the steps' range (2^-11 of it down
 // to 2^-29 of that, so that a long row's many small probabilities keep their
-// weight).  The sum l of the softmax is formed from 2^(s - m) in fp32.
+// weight; where the largest is below 2^-111, down to 2^-140).  The factor 2^-E of the end
+// is taken from the same E.  The sum l of the softmax is formed from 2^(s - m) in fp32.
 // Queries are scaled by a power of two to at most 1 and rounded to fp16 (exact
 // for unrotated fp16 and bf16 rows but for values below 2^-24 of the row's
 // largest); rotated ones are split in two fp16 parts (22 bits).
@@ -345,7 +346,8 @@ struct AttnKv4 {
 };
 
 constexpr int kTile = 64;        // tokens of one step of a wave
-constexpr float kShift = 15.0f;  // log2 of P' at its largest
+// E of a value maximum (2^E is finite, and so is the product with a probability).
+__device__ __forceinline__ float value_exp(float mv) { return fminf(15.0f - mv, 126.0f); }
 
 __device__ __forceinline__ uint32_t and_xor(uint32_t a, uint32_t m, uint32_t x) { return (a & m) ^ x; }
 
@@ -673,33 +675,37 @@ __global__ __launch_bounds__(64 * W, QT == 1 ? D < 256 ? 3 : 2 : 1) void attn_kv
 #pragma unroll
       for (int i = 0; i < SV; ++i)
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          top = fmaxf(top, c[i][e]);
-          topv = fmaxf(topv, fmaf(c[i][e], qscale[t], __builtin_amdgcn_logf(vs[i][e])));
-        }
+        for (int e = 0; e < 4; ++e) top = fmaxf(top, c[i][e]);
       top = row_max<RC>(top);
+      const float mn = fmaxf(m[t], top * qscale[t]);
+      const float mr = mn == -INFINITY ? 0.0f : mn;
+#pragma unroll
+      for (int i = 0; i < SV; ++i)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          c[i][e] = fmaf(c[i][e], qscale[t], -mr);
+          topv = fmaxf(topv, c[i][e] + __builtin_amdgcn_logf(vs[i][e]));
+        }
       topv = row_max<RC>(topv);
-      const float mn = fmaxf(m[t], top * qscale[t]), mvn = fmaxf(mv[t], topv);
-      const float mr = mn == -INFINITY ? 0.0f : mn, mvr = mvn == -INFINITY ? 0.0f : mvn;
-      // (At most 2^120, and times the probability first: 0 if that has underflowed,
-      // whatever the step.)
-      const float f = __builtin_amdgcn_exp2f(fminf(mr - mvr + kShift, 120.0f));
-      if (__builtin_amdgcn_ballot_w64(mn > m[t] || mvn > mv[t]) != 0) {
+      const float mvo = mv[t] + (m[t] - mr), mvn = fmaxf(mvo, topv), x = value_exp(mvn);
+      if (__builtin_amdgcn_ballot_w64(mn > m[t] || mvn > mvo) != 0) {
         l[t] *= __builtin_amdgcn_exp2f(m[t] - mr);
-        const float al = __builtin_amdgcn_exp2f(mv[t] - mvr);
+        const float al = __builtin_amdgcn_exp2f(m[t] - mr + x - value_exp(mv[t]));
         m[t] = mn;
         mv[t] = mvn;
 #pragma unroll
         for (int p = 0; p < PT; ++p)
 #pragma unroll
-          for (int x = 0; x < 2; ++x) acc[t][p][x] *= al;
+          for (int y = 0; y < 2; ++y) acc[t][p][y] *= al;
       }
+      // (Times the probability first: 0 if that has underflowed, whatever the step.)
+      const float f = __builtin_amdgcn_exp2f(x);
 #pragma unroll
       for (int i = 0; i < SV; ++i) {
         float p[4];
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-          p[e] = __builtin_amdgcn_exp2f(fmaf(c[i][e], qscale[t], -mr));
+          p[e] = __builtin_amdgcn_exp2f(c[i][e]);
           l[t] += p[e];
           p[e] = p[e] * f * vs[i][e];
         }
@@ -757,7 +763,7 @@ __global__ __launch_bounds__(64 * W, QT == 1 ? D < 256 ? 3 : 2 : 1) void attn_kv
             v4f{acc[t][p][0][2 * x], acc[t][p][1][2 * x], acc[t][p][0][2 * x + 1], acc[t][p][1][2 * x + 1]};
     if (g == 0) {
       sm[wave][16 * t + col][0] = m[t];
-      sm[wave][16 * t + col][1] = mv[t];
+      sm[wave][16 * t + col][1] = value_exp(mv[t]);
       sm[wave][16 * t + col][2] = s;
     }
   }
@@ -765,23 +771,24 @@ __global__ __launch_bounds__(64 * W, QT == 1 ? D < 256 ? 3 : 2 : 1) void attn_kv
   constexpr int TPR = D / 8;
   for (int i = threadIdx.x; i < min(OROWS, rows - r0) * TPR; i += 64 * W) {
     const int r = i / TPR, c = (i % TPR) * 8;
-    float M = -INFINITY, MV = -INFINITY;
+    float M = -INFINITY, X = INFINITY;
 #pragma unroll
-    for (int w = 0; w < W; ++w) {
-      M = fmaxf(M, sm[w][r][0]);
-      MV = fmaxf(MV, sm[w][r][1]);
-    }
-    const float mr = M == -INFINITY ? 0.0f : M, mvr = MV == -INFINITY ? 0.0f : MV;
+    for (int w = 0; w < W; ++w) M = fmaxf(M, sm[w][r][0]);
+    // A wave's outputs are 2^(its exponent + mr - its maximum) times too large; the least of these is
+    // at most 126 (that of a wave with the row's maximum), unless no wave has a token.
+    const float mr = M == -INFINITY ? 0.0f : M;
+#pragma unroll
+    for (int w = 0; w < W; ++w) X = fminf(X, sm[w][r][1] + (mr - sm[w][r][0]));
+    const float xr = X == INFINITY ? 0.0f : X;
     float L_ = 0.0f, y[8] = {};
 #pragma unroll
     for (int w = 0; w < W; ++w) {
       L_ += sm[w][r][2] * __builtin_amdgcn_exp2f(sm[w][r][0] - mr);
-      const float f = __builtin_amdgcn_exp2f(sm[w][r][1] - mvr);
+      const float f = __builtin_amdgcn_exp2f(xr - (sm[w][r][1] + (mr - sm[w][r][0])));
 #pragma unroll
       for (int e = 0; e < 8; ++e) y[e] += so[w][r][c + e] * f;
     }
-    // (No value maximum: every value that the row sees has step 0.)
-    const float f = L_ > 0.0f && MV > -INFINITY ? __builtin_amdgcn_exp2f(mvr - mr - kShift) / L_ : 0.0f;
+    const float f = L_ > 0.0f ? __builtin_amdgcn_exp2f(-xr) / L_ : 0.0f;
 #pragma unroll
     for (int e = 0; e < 8; ++e) y[e] *= f;
     const int64_t tok = q0 + (r0 + r) / a.R;

@@ -1,5 +1,6 @@
 """Attention over the 4-bit cache where its numbers are extreme: rows of zero
-values under strongly negative scores.  All expected values are float64's."""
+values under strongly negative scores, values near the smallest normal numbers.
+All expected values are float64's."""
 import pytest
 import torch
 
@@ -59,3 +60,28 @@ def test_zero_values_beside_others(L, start, stop, nq, dtype):
             ref, spread, _ = R.attend(q[:, h].double(), kk[:, h // 2], vv[:, h // 2], below, see)
             # (The other tokens' keys have step 0: their scores are 0 exactly.)
             R.check(o[:, h], ref, spread, 2.0 ** -18, dtype, 2.0 ** -11)
+
+
+@pytest.mark.parametrize("e", [100, 104, 106, 110, 116, 122])
+@pytest.mark.parametrize("L,nq,hq,d", [(1, 1, 2, 64), (64, 3, 4, 128), (700, 1, 8, 128), (6000, 2, 2, 256), (900, 12, 4, 64)])
+def test_small_steps(L, nq, hq, d, e):
+    """Steps of 2^-e, alone and among steps of up to 2^20 times as much.  2^126 of the
+    largest contribution is above 2^3, so that a contribution has fp16's 11 bits down to 2^-17 of it."""
+    g = torch.Generator().manual_seed(L + e)
+    for spread in (0, 20):
+        q, k = torch.randn((nq, hq, d), generator=g).bfloat16(), torch.randn((L, 2, d), generator=g).bfloat16()
+        v = torch.randint(-7, 8, (L, 2, d), generator=g).double()
+        v[:, :, 1] = 7.0
+        v = (v * 2.0 ** (torch.randint(0, spread + 1, (L, 1, 1), generator=g) - e)).bfloat16()
+        o, kk, vv = _call(q, k, v, 0.125)
+        see = torch.arange(L)[None, :] <= (L - nq + torch.arange(nq))[:, None]
+        for h in range(hq):
+            qq, one = q[:, h].double(), kk[:, h // (hq // 2)]
+            ref, size, p = R.attend(qq, one, vv[:, h // (hq // 2)], 0.125, see)
+            # The accumulator starts at 72 sum(q) in units of the step (max / 7).
+            extra = 2 * R.score_error(qq, one, 0.125)
+            extra += 2 * 0.125 * qq.abs().sum(-1).max().item() * one.abs().max().item() / 7 * 80 * (d + 8) * 2.0 ** -24
+            # ... and below that a contribution is off by half of fp16's smallest step, 2^-25, over 2^126, times 7
+            # (size is taken times 2^-10).
+            size = size + 7 * see.sum(-1, keepdim=True) * 2.0 ** -141
+            R.check(o[:, h], ref, size, extra, torch.bfloat16, 2.0 ** -11)
