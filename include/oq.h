@@ -432,8 +432,8 @@ int oq_w8a8_gemm_i32(const int8_t* Xq8, int64_t M, const int8_t* Wq8, int64_t N,
  * O        device [tokens][ldo] of dtype, ldo % 8 == 0; may not overlap Q, K, V
  * Probabilities are rounded to dtype for the second product (fp16: normal numbers
  * down to 2^-29 of a row's largest); sums and statistics are fp32.  Q, K and V of the
- * sequences' rows are finite: one that is not may show in any row of its sequence,
- * and in no other sequence.  About tokens / 128 + n_seqs workgroups a head, of 2^32
+ * sequences' rows are finite, and so are their products q . k in fp32: one that is not may
+ * show in any row of its sequence, and in no other sequence.  About tokens / 128 + n_seqs workgroups a head, of 2^32
  * threads at most together (OQ_ERR_SHAPE).
  * Errors: OQ_ERR_NULL, OQ_ERR_SHAPE, OQ_ERR_ALIGN, OQ_ERR_ARG, OQ_ERR_DEVICE,
  * OQ_ERR_HIP.
