@@ -324,7 +324,9 @@ __global__ __launch_bounds__(256) void kv4_gather_kernel(Cache c, const int64_t*
 // relative to the largest contribution whatever the steps' range (2^-11 of it down
 // to 2^-29 of that, so that a long row's many small probabilities keep their
 // weight; where the largest is below 2^-111, down to 2^-140).  The factor 2^-E of the end
-// is taken from the same E.  The sum l of the softmax is formed from 2^(s - m) in fp32.
+// is taken from the same E.  The sum l of the softmax is formed from 2^(s - m) in fp32.  m is kept
+// before the row's factor c, and 2^(s - m) is formed from s c - RN(m c) in one multiply-add as long as m c
+// is below 2^20, past which that rounding would decide; (s - m) c is used there.
 // Queries are scaled by a power of two to at most 1 and rounded to fp16 (exact
 // for unrotated fp16 and bf16 rows but for values below 2^-24 of the row's
 // largest); rotated ones are split in two fp16 parts (22 bits).
@@ -346,6 +348,7 @@ struct AttnKv4 {
 };
 
 constexpr int kTile = 64;        // tokens of one step of a wave
+constexpr float kFar = 0x1p20f;  // where the rounding of m c counts
 // E of a value maximum (2^E is finite, and so is the product with a probability).
 __device__ __forceinline__ float value_exp(float mv) { return fminf(15.0f - mv, 126.0f); }
 
@@ -420,6 +423,7 @@ __global__ __launch_bounds__(64 * W, QT == 1 ? D < 256 ? 3 : 2 : 1) void attn_kv
   struct Out {
     float o[W][OROWS][D + 4];
     float m[W][OROWS][3];
+    float c[OROWS];
   };
   __shared__ __attribute__((aligned(16))) union {
     Walk walk;
@@ -677,8 +681,17 @@ __global__ __launch_bounds__(64 * W, QT == 1 ? D < 256 ? 3 : 2 : 1) void attn_kv
 #pragma unroll
         for (int e = 0; e < 4; ++e) top = fmaxf(top, c[i][e]);
       top = row_max<RC>(top);
-      const float mn = fmaxf(m[t], top * qscale[t]);
-      const float mr = mn == -INFINITY ? 0.0f : mn;
+      const float mn = fmaxf(m[t], top), ms = mn * qscale[t];
+      float mr = ms, down = (m[t] - mn) * qscale[t];  // (log2 of what earlier sums shrink by)
+      if (__builtin_amdgcn_ballot_w64(fabsf(ms) >= kFar) != 0) {
+        const bool none = mn == -INFINITY, far = fabsf(ms) >= kFar && !none;
+        mr = none || far ? 0.0f : ms;
+        down = none ? -INFINITY : down;
+#pragma unroll
+        for (int i = 0; i < SV; ++i)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) c[i][e] -= far ? mn : 0.0f;
+      }
 #pragma unroll
       for (int i = 0; i < SV; ++i)
 #pragma unroll
@@ -687,10 +700,10 @@ __global__ __launch_bounds__(64 * W, QT == 1 ? D < 256 ? 3 : 2 : 1) void attn_kv
           topv = fmaxf(topv, c[i][e] + __builtin_amdgcn_logf(vs[i][e]));
         }
       topv = row_max<RC>(topv);
-      const float mvo = mv[t] + (m[t] - mr), mvn = fmaxf(mvo, topv), x = value_exp(mvn);
+      const float mvo = mv[t] + down, mvn = fmaxf(mvo, topv), x = value_exp(mvn);
       if (__builtin_amdgcn_ballot_w64(mn > m[t] || mvn > mvo) != 0) {
-        l[t] *= __builtin_amdgcn_exp2f(m[t] - mr);
-        const float al = __builtin_amdgcn_exp2f(m[t] - mr + x - value_exp(mv[t]));
+        l[t] *= __builtin_amdgcn_exp2f(down);
+        const float al = __builtin_amdgcn_exp2f(down + x - value_exp(mv[t]));
         m[t] = mn;
         mv[t] = mvn;
 #pragma unroll
@@ -765,6 +778,7 @@ __global__ __launch_bounds__(64 * W, QT == 1 ? D < 256 ? 3 : 2 : 1) void attn_kv
       sm[wave][16 * t + col][0] = m[t];
       sm[wave][16 * t + col][1] = value_exp(mv[t]);
       sm[wave][16 * t + col][2] = s;
+      if (wave == 0) smem.out.c[16 * t + col] = qscale[t];
     }
   }
   __syncthreads();
@@ -774,17 +788,21 @@ __global__ __launch_bounds__(64 * W, QT == 1 ? D < 256 ? 3 : 2 : 1) void attn_kv
     float M = -INFINITY, X = INFINITY;
 #pragma unroll
     for (int w = 0; w < W; ++w) M = fmaxf(M, sm[w][r][0]);
-    // A wave's outputs are 2^(its exponent + mr - its maximum) times too large; the least of these is
-    // at most 126 (that of a wave with the row's maximum), unless no wave has a token.
-    const float mr = M == -INFINITY ? 0.0f : M;
+    // A wave's outputs are 2^(its exponent - down) times too large; the least of these is at
+    // most 126 (that of a wave with the row's maximum), unless no wave has a token.
+    const float mr = M == -INFINITY ? 0.0f : M, qs = smem.out.c[r];
+    float down[W];
 #pragma unroll
-    for (int w = 0; w < W; ++w) X = fminf(X, sm[w][r][1] + (mr - sm[w][r][0]));
+    for (int w = 0; w < W; ++w) {
+      down[w] = (sm[w][r][0] - mr) * qs;
+      X = fminf(X, sm[w][r][1] - down[w]);
+    }
     const float xr = X == INFINITY ? 0.0f : X;
     float L_ = 0.0f, y[8] = {};
 #pragma unroll
     for (int w = 0; w < W; ++w) {
-      L_ += sm[w][r][2] * __builtin_amdgcn_exp2f(sm[w][r][0] - mr);
-      const float f = __builtin_amdgcn_exp2f(xr - (sm[w][r][1] + (mr - sm[w][r][0])));
+      L_ += sm[w][r][2] * __builtin_amdgcn_exp2f(down[w]);
+      const float f = __builtin_amdgcn_exp2f(xr - (sm[w][r][1] - down[w]));
 #pragma unroll
       for (int e = 0; e < 8; ++e) y[e] += so[w][r][c + e] * f;
     }
@@ -799,12 +817,12 @@ __global__ __launch_bounds__(64 * W, QT == 1 ? D < 256 ? 3 : 2 : 1) void attn_kv
       float* o = a.part + ((tok * a.hq + head) * a.splits + split) * (D + 4);
       *reinterpret_cast<float4*>(o + c) = make_float4(y[0], y[1], y[2], y[3]);
       *reinterpret_cast<float4*>(o + c + 4) = make_float4(y[4], y[5], y[6], y[7]);
-      if (c == 0) *reinterpret_cast<float2*>(o + D) = make_float2(M, L_);
+      if (c == 0) *reinterpret_cast<float4*>(o + D) = make_float4(M, L_, qs, 0.0f);
     }
   }
 }
 
-// o = sum_s w_s o_s / sum_s w_s with w_s = l_s 2^(m_s - m).  A row (token and head)
+// o = sum_s w_s o_s / sum_s w_s with w_s = l_s 2^((m_s - m) c).  A row (token and head)
 // has WPR waves, 8 channels a thread; its splits are dealt to their 64 WPR / (D / 8)
 // groups of threads.
 template <int D, int WPR, bool BF>
@@ -822,14 +840,15 @@ __global__ __launch_bounds__(256) void attn_kv4_join_kernel(AttnKv4 a) {
   const int64_t tok = q0 + blockIdx.y;
   const int c = (tid % TPR) * 8, grp = tid / TPR;
   const float* p = a.part + (tok * a.hq + min(head, a.hq - 1)) * a.splits * (D + 4);
-  float M = -INFINITY, W = 0.0f, y[8] = {};
+  float M = -INFINITY, W = 0.0f, qs = 1.0f, y[8] = {};
 #pragma unroll 4
   for (int s = grp; s < splits; s += G) {
     const float* ps = p + s * (D + 4);
-    const float2 ml = *reinterpret_cast<const float2*>(ps + D);
+    const float4 ml = *reinterpret_cast<const float4*>(ps + D);
     const float4 u = *reinterpret_cast<const float4*>(ps + c), v = *reinterpret_cast<const float4*>(ps + c + 4);
     const float mn = fmaxf(M, ml.x), mr = mn == -INFINITY ? 0.0f : mn;
-    const float al = __builtin_amdgcn_exp2f(M - mr), w = ml.y * __builtin_amdgcn_exp2f(ml.x - mr);
+    qs = ml.z;
+    const float al = __builtin_amdgcn_exp2f((M - mr) * qs), w = ml.y * __builtin_amdgcn_exp2f((ml.x - mr) * qs);
     const float x[8] = {u.x, u.y, u.z, u.w, v.x, v.y, v.z, v.w};
     M = mn;
     W = W * al + w;
@@ -851,7 +870,7 @@ __global__ __launch_bounds__(256) void attn_kv4_join_kernel(AttnKv4 a) {
   float T = 0.0f, z[8] = {};
 #pragma unroll 4
   for (int i = 0; i < G; ++i) {
-    const float w = __builtin_amdgcn_exp2f(sy[sub][i][D] - mr);
+    const float w = __builtin_amdgcn_exp2f((sy[sub][i][D] - mr) * qs);
     T += sy[sub][i][D + 1] * w;
 #pragma unroll
     for (int e = 0; e < 8; ++e) z[e] += sy[sub][i][c + e] * w;

@@ -1,5 +1,6 @@
 """Attention over the 4-bit cache where its numbers are extreme: rows of zero
-values under strongly negative scores, values near the smallest normal numbers.
+values under strongly negative scores, values near the smallest normal numbers,
+scores far past 2^24.
 All expected values are float64's."""
 import pytest
 import torch
@@ -85,3 +86,48 @@ def test_small_steps(L, nq, hq, d, e):
             # (size is taken times 2^-10).
             size = size + 7 * see.sum(-1, keepdim=True) * 2.0 ** -141
             R.check(o[:, h], ref, size, extra, torch.bfloat16, 2.0 ** -11)
+
+
+@pytest.mark.parametrize("dtype,q0,step,high,low", [
+    (torch.float16, 700.0, 97.0, 1000.0, 500.0),
+    (torch.float16, -20000.0, 1024.0, 29000.0, 30000.0),
+    (torch.bfloat16, 700.0, 97.0, 1000.0, 500.0),
+    (torch.bfloat16, 2.0 ** 30, 2.0 ** 27, 2.0 ** 30, 2.0 ** 29),
+    (torch.bfloat16, -2.0 ** 30, -2.0 ** 27, 2.0 ** 29, 2.0 ** 30),
+])
+@pytest.mark.parametrize("L,nq,hq,d,rotate", [(1, 1, 2, 64, False), (300, 3, 4, 128, False), (300, 20, 2, 64, True), (700, 5, 8, 256, False),
+                                              (6000, 1, 4, 128, True), (6000, 9, 2, 64, False), (3000, 20, 4, 128, False)])
+def test_equal_large_scores(L, nq, hq, d, rotate, dtype, q0, step, high, low):
+    """Keys that share the largest score share the weight, however large it is."""
+    q = (q0 + step * torch.arange(nq * hq).view(nq, hq, 1)).expand(nq, hq, d).to(dtype).contiguous()
+    k = torch.full((L, 2, d), low, dtype=dtype)
+    k[::2] = high
+    v = torch.randn((L, 2, d), generator=torch.Generator().manual_seed(L)).to(dtype)
+    o, kk, vv = _call(q, k, v, d ** -0.5, rotate)
+    see = torch.arange(L)[None, :] <= (L - nq + torch.arange(nq))[:, None]
+    for h in range(hq):
+        qq = q[:, h].double()
+        ref, spread, _ = R.attend(qq @ R.hadamard(d) / d ** 0.5 if rotate else qq, kk[:, h // (hq // 2)], vv[:, h // (hq // 2)],
+                                  d ** -0.5, see)
+        # (Equal keys have equal scores, whatever they were rounded to; the others are too far below to count.)
+        R.check(o[:, h], ref, spread, 2.0 ** -15, dtype, 2.0 ** -11)
+
+
+@pytest.mark.parametrize("dtype", [torch.float16, torch.bfloat16])
+@pytest.mark.parametrize("L", [300, 6000])
+def test_maxima_that_grow(L, dtype):
+    """Scores that double along the sequence, from 2^-3 to 2^29 and from -2^29 up."""
+    d = 64
+    v = torch.randn((L, 1, d), generator=torch.Generator().manual_seed(3)).to(dtype)
+    for down in (False, True):
+        q, k = torch.zeros((1, 3, d), dtype=dtype), torch.zeros((L, 1, d), dtype=dtype)
+        q[:, :, 0] = 2.0 ** 15
+        k[:, 0, 0] = 2.0 ** (torch.arange(L) * (33.0 / L) - 18).floor()
+        if down:
+            k = -k.flip(0)
+        o, kk, vv = _call(q, k, v, 1.0)
+        ref, spread, _ = R.attend(q[:, 0].double(), kk[:, 0], vv[:, 0], 1.0, torch.ones((1, L), dtype=torch.bool))
+        # (Where several scores count they are below 2^6; the product, the step's and the factor's roundings and the
+        # exponent's are four of 2^-24 of 2^6.5, which counts twice.)
+        for h in range(3):
+            R.check(o[:, h], ref, spread, 2.0 ** -14, dtype, 2.0 ** -11)
