@@ -560,8 +560,9 @@ __global__ __launch_bounds__(64 * W, QT == 1 ? D < 256 ? 3 : 2 : 1) void attn_kv
       if constexpr (TQ > 8) sum += rqd::lane_xor_dpp<8>(sum);
       if (part == 0) {
         sqc[qr][0] = -72.0f * sum;
-        // (Above 0, so that a masked score of -inf times it is -inf.)
-        sqc[qr][1] = fmaxf(ldexpf(a.scale_log2e * norm, e), 1e-38f);
+        // (Above 0, so that a masked score of -inf times it is -inf, though by no more than fp32's smallest number:
+        // keys may be as large as the query is small.)
+        sqc[qr][1] = fmaxf(ldexpf(a.scale_log2e * norm, e), 0x1p-149f);
       }
     }
   }

@@ -131,3 +131,26 @@ def test_maxima_that_grow(L, dtype):
         # exponent's are four of 2^-24 of 2^6.5, which counts twice.)
         for h in range(3):
             R.check(o[:, h], ref, spread, 2.0 ** -14, dtype, 2.0 ** -11)
+
+
+@pytest.mark.parametrize("rotate", [False, True])
+@pytest.mark.parametrize("e", [120, 126, 130, 133])
+def test_small_queries_and_large_keys(e, rotate):
+    """Queries down to bf16's smallest number against keys of up to 2^126: the
+    row's factor is below fp32's normal numbers, the scores are not."""
+    d, L = 64, 100
+    q, k = torch.zeros((2, 2, d), dtype=torch.bfloat16), torch.zeros((L, 1, d), dtype=torch.bfloat16)
+    q[:, 0, 3], q[:, 1, 5] = 2.0 ** -e, -(2.0 ** -e)
+    k[:, 0, 3], k[:, 0, 5] = 2.0 ** (e - 8), 2.0 ** (e - 9)
+    k[::3] = -k[::3]
+    v = torch.randn((L, 1, d), generator=torch.Generator().manual_seed(e)).bfloat16()
+    o, kk, vv = _call(q, k, v, 32.0, rotate, causal=False)
+    o2, _, _ = _call(q, k, v, 0.25, rotate, causal=False)
+    for scale, got in ((32.0, o), (0.25, o2)):
+        for h in range(2):
+            qq = q[:, h].double()
+            qq = qq @ R.hadamard(d) / d ** 0.5 if rotate else qq
+            ref, spread, _ = R.attend(qq, kk[:, 0], vv[:, 0], scale, torch.ones((2, L), dtype=torch.bool))
+            # (2^-10: the factor has 11 bits at least.  The start of 72 sum(q) and 22 bits of a rotated query are below it.)
+            extra = 2 * R.score_error(qq, kk[:, 0], scale) + 2.0 ** -9 * scale * (qq.abs() @ kk[:, 0].abs().T).max().item()
+            R.check(got[:, h], ref, spread, extra, torch.bfloat16, 2.0 ** -11)
