@@ -3,7 +3,8 @@
 Thin marshalling layer over the C ABI in include/oq.h: every computation runs
 in the library's HIP kernels; torch only provides device memory and the
 stream.  Functions have the names of the C entry points without the ``oq_``
-prefix.  Raises OQError on a non-zero status.
+prefix; memory that a call with ``stream=`` makes is of that stream.  Raises
+OQError on a non-zero status.
 """
 from __future__ import annotations
 
@@ -53,6 +54,16 @@ def _on(stream, dev):
     return _raw_stream(dev) if stream is None and _raw_stream is not None else _stream(stream)
 
 
+def _empty(t, shape, dtype, stream):
+    """Memory for a call's outputs and workspaces, on t's device.  That of a call
+    on a given stream is of this stream, as under torch.cuda.stream: the current
+    one may still read what it was before, and may hand it out again early."""
+    if stream is None:
+        return t.new_empty(shape, dtype=dtype)
+    with torch.cuda.stream(stream):
+        return t.new_empty(shape, dtype=dtype)
+
+
 def _ld(t):
     """Leading dimension (elements from one row to the next) of a 2-D tensor.
     The stride of a single row is unconstrained (numpy and torch may give it
@@ -88,9 +99,9 @@ def rotate_quantize_act(X, had_block, s_table=None, t=0, Xq=None, x_scale=None, 
     """X: fp16 [M, K] (row stride X.stride(0); any stride for a single row).  Returns (Xq uint8 [M, K/2], x_scale f32 [M])."""
     M, K = X.shape
     if Xq is None:
-        Xq = torch.empty((M, K // 2), dtype=torch.uint8, device=X.device)
+        Xq = _empty(X, (M, K // 2), torch.uint8, stream)
     if x_scale is None:
-        x_scale = torch.empty((M,), dtype=torch.float32, device=X.device)
+        x_scale = _empty(X, (M,), torch.float32, stream)
     keep, sp = _s_table(s_table)
     _check(lib().oq_rotate_quantize_act(_ptr(X), M, K, _ld(X), had_block, sp, t, _ptr(Xq),
                                         _ptr(x_scale), _stream(stream)), "oq_rotate_quantize_act")
@@ -107,9 +118,9 @@ def rotate_quantize_act_tiled(X, had_block, s_table=None, t=0, Xt=None, x_scale=
     """As rotate_quantize_act, codes in the 16-row tiled layout (uint8 [tiled_bytes(M, K)])."""
     M, K = X.shape
     if Xt is None:
-        Xt = torch.empty((tiled_bytes(M, K),), dtype=torch.uint8, device=X.device)
+        Xt = _empty(X, (tiled_bytes(M, K),), torch.uint8, stream)
     if x_scale is None:
-        x_scale = torch.empty((M,), dtype=torch.float32, device=X.device)
+        x_scale = _empty(X, (M,), torch.float32, stream)
     keep, sp = _s_table(s_table)
     _check(lib().oq_rotate_quantize_act_tiled(_ptr(X), M, K, _ld(X), had_block, sp, t, _ptr(Xt),
                                               _ptr(x_scale), _stream(stream)), "oq_rotate_quantize_act_tiled")
@@ -122,7 +133,7 @@ def codes_to_tiled(Q, K=None, T=None, stream=None):
     R, Kh = Q.shape
     K = 2 * Kh if K is None else K
     if T is None:
-        T = torch.empty((tiled_bytes(R, K),), dtype=torch.uint8, device=Q.device)
+        T = _empty(Q, (tiled_bytes(R, K),), torch.uint8, stream)
     _check(lib().oq_codes_to_tiled(_ptr(Q), R, K, _ptr(T), _stream(stream)), "oq_codes_to_tiled")
     return T
 
@@ -134,9 +145,9 @@ def rotate_quantize_act_composite(X, perm, Rt, s_table=None, t=0, Xq=None, x_sca
     Returns (Xq uint8 [M, K/2], x_scale f32 [M])."""
     M, K = X.shape
     if Xq is None:
-        Xq = torch.empty((M, K // 2), dtype=torch.uint8, device=X.device)
+        Xq = _empty(X, (M, K // 2), torch.uint8, stream)
     if x_scale is None:
-        x_scale = torch.empty((M,), dtype=torch.float32, device=X.device)
+        x_scale = _empty(X, (M,), torch.float32, stream)
     keep, sp = _s_table(s_table)
     _check(lib().oq_rotate_quantize_act_composite(_ptr(X), M, K, _ld(X), _ptr(perm), _ptr(Rt), sp, t,
                                                   _ptr(Xq), _ptr(x_scale), _stream(stream)),
@@ -181,8 +192,8 @@ def quantize_weights_composite_host(W_u: np.ndarray, perm: np.ndarray, Rt: np.nd
 def rotate_debug_f32(X, had_block, s_table=None, t=0, stream=None):
     """Pre-rounding ratios z/Delta (f32 [M, K]) and x_scale."""
     M, K = X.shape
-    ratio = torch.empty((M, K), dtype=torch.float32, device=X.device)
-    x_scale = torch.empty((M,), dtype=torch.float32, device=X.device)
+    ratio = _empty(X, (M, K), torch.float32, stream)
+    x_scale = _empty(X, (M,), torch.float32, stream)
     keep, sp = _s_table(s_table)
     _check(lib().oq_rotate_debug_f32(_ptr(X), M, K, _ld(X), had_block, sp, t, _ptr(ratio),
                                      _ptr(x_scale), _stream(stream)), "oq_rotate_debug_f32")
@@ -197,7 +208,7 @@ def w4a4_linear(Xq, x_scale, Wq, w_scale, bias=None, out_dtype=OUT_F16, Y=None, 
     K = 2 * Kh
     if Y is None:
         dt = torch.float16 if out_dtype == OUT_F16 else torch.bfloat16
-        Y = torch.empty((M, N), dtype=dt, device=Xq.device)
+        Y = _empty(Xq, (M, N), dt, stream)
     _check(lib().oq_w4a4_linear(_ptr(Xq), _ptr(x_scale), M, _ptr(Wq), _ptr(w_scale), _ptr(bias), N, K,
                                 _ptr(Y), _ld(Y), out_dtype, _stream(stream)), "oq_w4a4_linear")
     return Y
@@ -207,7 +218,7 @@ def w4a4_gemm_i32(Xq, Wq, acc=None, stream=None):
     M = Xq.shape[0]
     N, Kh = Wq.shape
     if acc is None:
-        acc = torch.empty((M, N), dtype=torch.int32, device=Xq.device)
+        acc = _empty(Xq, (M, N), torch.int32, stream)
     _check(lib().oq_w4a4_gemm_i32(_ptr(Xq), M, _ptr(Wq), N, 2 * Kh, _ptr(acc), _ld(acc),
                                   _stream(stream)), "oq_w4a4_gemm_i32")
     return acc
@@ -220,7 +231,7 @@ def w4a4_linear_tiled(Xt, x_scale, Wq, w_scale, bias=None, out_dtype=OUT_F16, Y=
     K = 2 * Kh
     if Y is None:
         dt = torch.float16 if out_dtype == OUT_F16 else torch.bfloat16
-        Y = torch.empty((M, N), dtype=dt, device=Wq.device)
+        Y = _empty(Wq, (M, N), dt, stream)
     _check(lib().oq_w4a4_linear_tiled(_ptr(Xt), _ptr(x_scale), M, _ptr(Wq), _ptr(w_scale), _ptr(bias), N, K,
                                       _ptr(Y), _ld(Y), out_dtype, _stream(stream)), "oq_w4a4_linear_tiled")
     return Y
@@ -229,7 +240,7 @@ def w4a4_linear_tiled(Xt, x_scale, Wq, w_scale, bias=None, out_dtype=OUT_F16, Y=
 def w4a4_gemm_i32_tiled(Xt, M, Wq, acc=None, stream=None):
     N, Kh = Wq.shape
     if acc is None:
-        acc = torch.empty((M, N), dtype=torch.int32, device=Wq.device)
+        acc = _empty(Wq, (M, N), torch.int32, stream)
     _check(lib().oq_w4a4_gemm_i32_tiled(_ptr(Xt), M, _ptr(Wq), N, 2 * Kh, _ptr(acc), _ld(acc),
                                         _stream(stream)), "oq_w4a4_gemm_i32_tiled")
     return acc
@@ -239,9 +250,9 @@ def quantize_weights(W_u, had_block, Wq=None, w_scale=None, stream=None):
     """W_u fp16 [N, K] on the device -> (Wq uint8 [N, K/2], w_scale f32 [N])."""
     N, K = W_u.shape
     if Wq is None:
-        Wq = torch.empty((N, K // 2), dtype=torch.uint8, device=W_u.device)
+        Wq = _empty(W_u, (N, K // 2), torch.uint8, stream)
     if w_scale is None:
-        w_scale = torch.empty((N,), dtype=torch.float32, device=W_u.device)
+        w_scale = _empty(W_u, (N,), torch.float32, stream)
     _check(lib().oq_quantize_weights(_ptr(W_u), N, K, _ld(W_u), had_block, _ptr(Wq), _ptr(w_scale),
                                      _stream(stream)), "oq_quantize_weights")
     return Wq, w_scale
@@ -262,9 +273,9 @@ def rotate_quantize_act_i8(X, had_block, s_table=None, t=0, Xq8=None, x_scale=No
     """W4A8 activation side: 8-bit per-token codes (int8 [M, K]) and x_scale f32 [M]."""
     M, K = X.shape
     if Xq8 is None:
-        Xq8 = torch.empty((M, K), dtype=torch.int8, device=X.device)
+        Xq8 = _empty(X, (M, K), torch.int8, stream)
     if x_scale is None:
-        x_scale = torch.empty((M,), dtype=torch.float32, device=X.device)
+        x_scale = _empty(X, (M,), torch.float32, stream)
     keep, sp = _s_table(s_table)
     _check(lib().oq_rotate_quantize_act_i8(_ptr(X), M, K, _ld(X), had_block, sp, t, _ptr(Xq8),
                                            _ptr(x_scale), _stream(stream)), "oq_rotate_quantize_act_i8")
@@ -278,7 +289,7 @@ def w4a8_linear(Xq8, x_scale, Wq, w_scale, bias=None, out_dtype=OUT_F16, Y=None,
     N = Wq.shape[0]
     if Y is None:
         dt = torch.float16 if out_dtype == OUT_F16 else torch.bfloat16
-        Y = torch.empty((M, N), dtype=dt, device=Xq8.device)
+        Y = _empty(Xq8, (M, N), dt, stream)
     _check(lib().oq_w4a8_linear(_ptr(Xq8), _ptr(x_scale), M, _ptr(Wq), _ptr(w_scale), _ptr(bias), N, K,
                                 _ptr(Y), _ld(Y), out_dtype, _stream(stream)), "oq_w4a8_linear")
     return Y
@@ -288,7 +299,7 @@ def w4a8_gemm_i32(Xq8, Wq, acc=None, stream=None):
     M, K = Xq8.shape
     N = Wq.shape[0]
     if acc is None:
-        acc = torch.empty((M, N), dtype=torch.int32, device=Xq8.device)
+        acc = _empty(Xq8, (M, N), torch.int32, stream)
     _check(lib().oq_w4a8_gemm_i32(_ptr(Xq8), M, _ptr(Wq), N, K, _ptr(acc), _ld(acc), _stream(stream)),
            "oq_w4a8_gemm_i32")
     return acc
@@ -298,9 +309,9 @@ def quantize_weights_i8(W_u, had_block, Wq8=None, w_scale=None, stream=None):
     """W_u fp16 [N, K] on the device -> (Wq8 int8 [N, K], w_scale f32 [N])."""
     N, K = W_u.shape
     if Wq8 is None:
-        Wq8 = torch.empty((N, K), dtype=torch.int8, device=W_u.device)
+        Wq8 = _empty(W_u, (N, K), torch.int8, stream)
     if w_scale is None:
-        w_scale = torch.empty((N,), dtype=torch.float32, device=W_u.device)
+        w_scale = _empty(W_u, (N,), torch.float32, stream)
     if W_u.dtype != torch.float16 or (K > 1 and W_u.stride(1) != 1):
         raise ValueError("W_u: float16 [N, K] rows expected")
     if (Wq8.shape != (N, K) or Wq8.dtype != torch.int8 or not Wq8.is_contiguous() or w_scale.shape != (N,)
@@ -341,7 +352,7 @@ def w8a8_linear(Xq8, x_scale, Wq8, w_scale, bias=None, out_dtype=OUT_F16, Y=None
         raise ValueError("bias: contiguous float16 [N] expected")
     dt = torch.float16 if out_dtype == OUT_F16 else torch.bfloat16
     if Y is None:
-        Y = Xq8.new_empty((M, N), dtype=dt)
+        Y = _empty(Xq8, (M, N), dt, stream)
     elif Y.shape != (M, N) or Y.dtype != dt or (N > 1 and Y.stride(1) != 1):
         raise ValueError("Y: [M, N] rows of out_dtype expected")
     dev = _one_gpu(Xq8, x_scale, Wq8, w_scale, Y) if bias is None else _one_gpu(Xq8, x_scale, Wq8, w_scale, Y, bias)
@@ -355,7 +366,7 @@ def w8a8_gemm_i32(Xq8, Wq8, acc=None, stream=None):
     N = Wq8.shape[0]
     _int8_operands(Xq8, Wq8)
     if acc is None:
-        acc = torch.empty((M, N), dtype=torch.int32, device=Xq8.device)
+        acc = _empty(Xq8, (M, N), torch.int32, stream)
     elif acc.shape != (M, N) or acc.dtype != torch.int32 or (N > 1 and acc.stride(1) != 1):
         raise ValueError("acc: int32 [M, N] rows expected")
     dev = _one_gpu(Xq8, Wq8, acc)
@@ -368,7 +379,7 @@ def channel_energy(W, energy=None, stream=None):
     """fp64 [K] column energies sum_n W[n][j]^2 of a device fp16 weight [N, K]."""
     N, K = W.shape
     if energy is None:
-        energy = torch.empty((K,), dtype=torch.float64, device=W.device)
+        energy = _empty(W, (K,), torch.float64, stream)
     _check(lib().oq_channel_energy(_ptr(W), N, K, _ld(W), _ptr(energy), _stream(stream)), "oq_channel_energy")
     return energy
 
@@ -377,7 +388,7 @@ def zigzag_permutation(energy, block=64, perm=None, stream=None):
     """Device zigzag permutation (int32 [K]) from device fp64 energies."""
     K = energy.shape[0]
     if perm is None:
-        perm = torch.empty((K,), dtype=torch.int32, device=energy.device)
+        perm = _empty(energy, (K,), torch.int32, stream)
     _check(lib().oq_zigzag_permutation(_ptr(energy), K, block, _ptr(perm), _stream(stream)), "oq_zigzag_permutation")
     return perm
 
@@ -387,9 +398,9 @@ def block_svd(W, perm, block=64, U=None, sigma2=None, stream=None):
     N, K = W.shape
     nb = K // block
     if U is None:
-        U = torch.empty((nb, block, block), dtype=torch.float64, device=W.device)
+        U = _empty(W, (nb, block, block), torch.float64, stream)
     if sigma2 is None:
-        sigma2 = torch.empty((nb, block), dtype=torch.float64, device=W.device)
+        sigma2 = _empty(W, (nb, block), torch.float64, stream)
     _check(lib().oq_block_svd(_ptr(W), N, K, _ld(W), _ptr(perm), block, _ptr(U), _ptr(sigma2),
                               _stream(stream)), "oq_block_svd")
     return U, sigma2
@@ -399,7 +410,7 @@ def block_rotations(U, Rt=None, stream=None):
     """fp16 column-major blocks (int16 [nb, 64, 64]) of U_b H_64 / 8."""
     nb, c, _ = U.shape
     if Rt is None:
-        Rt = torch.empty((nb, c, c), dtype=torch.int16, device=U.device)
+        Rt = _empty(U, (nb, c, c), torch.int16, stream)
     _check(lib().oq_block_rotations(_ptr(U), nb * c, c, _ptr(Rt), _stream(stream)), "oq_block_rotations")
     return Rt
 
@@ -408,13 +419,12 @@ def prepare_weights_composite(W, stream=None):
     """Device fp16 weight [N, K] -> (perm int32 [K], Rt int16 [K/64, 64, 64],
     Wq uint8 [N, K/2], w_scale f32 [N]), all on the device."""
     N, K = W.shape
-    dev = W.device
-    perm = torch.empty((K,), dtype=torch.int32, device=dev)
-    Rt = torch.empty((K // 64, 64, 64), dtype=torch.int16, device=dev)
-    Wq = torch.empty((N, K // 2), dtype=torch.uint8, device=dev)
-    ws = torch.empty((N,), dtype=torch.float32, device=dev)
+    perm = _empty(W, (K,), torch.int32, stream)
+    Rt = _empty(W, (K // 64, 64, 64), torch.int16, stream)
+    Wq = _empty(W, (N, K // 2), torch.uint8, stream)
+    ws = _empty(W, (N,), torch.float32, stream)
     nbytes = int(lib().oq_prepare_weights_workspace_bytes(K))
-    work = torch.empty((max(nbytes, 16),), dtype=torch.uint8, device=dev)
+    work = _empty(W, (max(nbytes, 16),), torch.uint8, stream)
     _check(lib().oq_prepare_weights_composite(_ptr(W), N, K, _ld(W), _ptr(perm), _ptr(Rt), _ptr(Wq), _ptr(ws),
                                               _ptr(work), work.numel(), _stream(stream)),
            "oq_prepare_weights_composite")
@@ -425,7 +435,7 @@ def rotate_act_f32(X, had_block, Y=None, stream=None):
     """Rotated activation y = x H_b / sqrt(b) in fp32 [M, K] (calibration input)."""
     M, K = X.shape
     if Y is None:
-        Y = torch.empty((M, K), dtype=torch.float32, device=X.device)
+        Y = _empty(X, (M, K), torch.float32, stream)
     _check(lib().oq_rotate_act_f32(_ptr(X), M, K, _ld(X), had_block, _ptr(Y), _stream(stream)),
            "oq_rotate_act_f32")
     return Y
@@ -439,9 +449,9 @@ def calibrate_step_scales(Y, p=99.9, qmax=7.0, delta=None, work=None, stream=Non
     """Static steps delta f32 [K] = nearest-rank p-th percentile of |Y[:, j]| / qmax."""
     n, K = Y.shape
     if delta is None:
-        delta = torch.empty((K,), dtype=torch.float32, device=Y.device)
+        delta = _empty(Y, (K,), torch.float32, stream)
     if work is None:
-        work = torch.empty((max(calibrate_workspace_bytes(K), 16),), dtype=torch.uint8, device=Y.device)
+        work = _empty(Y, (max(calibrate_workspace_bytes(K), 16),), torch.uint8, stream)
     _check(lib().oq_calibrate_step_scales(_ptr(Y), n, K, _ld(Y), float(p), float(qmax), _ptr(delta),
                                           _ptr(work), work.numel(), _stream(stream)), "oq_calibrate_step_scales")
     return delta
@@ -453,7 +463,7 @@ def calibrate_step_scales_noalloc(Y, p=99.9, qmax=7.0, delta=None, stream=None):
     here either)."""
     n, K = Y.shape
     if delta is None:
-        delta = torch.empty((K,), dtype=torch.float32, device=Y.device)
+        delta = _empty(Y, (K,), torch.float32, stream)
     _check(lib().oq_calibrate_step_scales_noalloc(_ptr(Y), n, K, _ld(Y), float(p), float(qmax), _ptr(delta),
                                                   _stream(stream)), "oq_calibrate_step_scales_noalloc")
     return delta
@@ -463,9 +473,9 @@ def rotate_quantize_act_static(X, had_block, delta, Xq=None, x_scale=None, strea
     """Rotation + static per-channel steps delta (f32 [K], device): (Xq uint8 [M, K/2], x_scale = 1)."""
     M, K = X.shape
     if Xq is None:
-        Xq = torch.empty((M, K // 2), dtype=torch.uint8, device=X.device)
+        Xq = _empty(X, (M, K // 2), torch.uint8, stream)
     if x_scale is None:
-        x_scale = torch.empty((M,), dtype=torch.float32, device=X.device)
+        x_scale = _empty(X, (M,), torch.float32, stream)
     _check(lib().oq_rotate_quantize_act_static(_ptr(X), M, K, _ld(X), had_block, _ptr(delta), _ptr(Xq),
                                                _ptr(x_scale), _stream(stream)), "oq_rotate_quantize_act_static")
     return Xq, x_scale
@@ -475,9 +485,9 @@ def rotate_quantize_act_static_tiled(X, had_block, delta, Xt=None, x_scale=None,
     """As rotate_quantize_act_static, codes in the 16-row tiled layout."""
     M, K = X.shape
     if Xt is None:
-        Xt = torch.empty((tiled_bytes(M, K),), dtype=torch.uint8, device=X.device)
+        Xt = _empty(X, (tiled_bytes(M, K),), torch.uint8, stream)
     if x_scale is None:
-        x_scale = torch.empty((M,), dtype=torch.float32, device=X.device)
+        x_scale = _empty(X, (M,), torch.float32, stream)
     _check(lib().oq_rotate_quantize_act_static_tiled(_ptr(X), M, K, _ld(X), had_block, _ptr(delta),
                                                      _ptr(Xt), _ptr(x_scale), _stream(stream)),
            "oq_rotate_quantize_act_static_tiled")
@@ -489,9 +499,9 @@ def quantize_weights_step(W_u, had_block, delta, Wq=None, w_scale=None, stream=N
     (f32 [K]) per input channel and RTN-quantized: (Wq uint8 [N, K/2], w_scale f32 [N])."""
     N, K = W_u.shape
     if Wq is None:
-        Wq = torch.empty((N, K // 2), dtype=torch.uint8, device=W_u.device)
+        Wq = _empty(W_u, (N, K // 2), torch.uint8, stream)
     if w_scale is None:
-        w_scale = torch.empty((N,), dtype=torch.float32, device=W_u.device)
+        w_scale = _empty(W_u, (N,), torch.float32, stream)
     _check(lib().oq_quantize_weights_step(_ptr(W_u), N, K, _ld(W_u), had_block, _ptr(delta), _ptr(Wq),
                                           _ptr(w_scale), _stream(stream)), "oq_quantize_weights_step")
     return Wq, w_scale

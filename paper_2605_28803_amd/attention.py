@@ -10,7 +10,7 @@ import ctypes as C
 
 import torch
 
-from . import _check, _current_device, _lib, _on, _ptr  # (the package has these before it imports this module)
+from . import _check, _current_device, _empty, _lib, _on, _ptr  # (the package has these before it imports this module)
 
 _DTYPE = {torch.float16: 0, torch.bfloat16: 1, torch.float32: 2}
 _TORCH = {0: torch.float16, 1: torch.bfloat16, 2: torch.float32}
@@ -67,7 +67,7 @@ def attention_prompt(Q, K, V, cu_seqlens, causal=True, scale=None, O=None, strea
     _want(n_cu >= 1, "cu_seqlens: at least one element expected")
     _ints(cu_seqlens, "cu_seqlens", torch.int32, n_cu, dev)
     if O is None:
-        O, ldo = Q.new_empty((T, hq, d)), hq * d
+        O, ldo = _empty(Q, (T, hq, d), Q.dtype, stream), hq * d
     else:
         _want(O.shape == Q.shape and O.dtype == Q.dtype and O.get_device() == dev, "O: Q's shape, type and device expected")
         ldo = _heads(O, "O", d)
@@ -141,8 +141,8 @@ def kv4_gather(cache, slots, out_dtype=0, K=None, V=None, stream=None):
         else:
             _want(t.shape == shape and t.dtype == dt and t.get_device() == dev, f"{name}: {list(shape)} of {dt} on cuda:{dev} expected")
             ld.append(_heads(t, name, shape[2]))
-    K = torch.empty(shape, dtype=dt, device=slots.device) if K is None else K
-    V = torch.empty(shape, dtype=dt, device=slots.device) if V is None else V
+    K = _empty(slots, shape, dt, stream) if K is None else K
+    V = _empty(slots, shape, dt, stream) if V is None else V
     _check(_lib.load().oq_kv4_gather(cache.ref, _ptr(slots), n, _ptr(K), _ptr(V), ld[0], ld[1], out_dtype,
                                      _on(stream, dev)), "oq_kv4_gather")
     return K, V
@@ -186,18 +186,13 @@ def attention_kv4(Q, cache, block_table, seq_lens, cu_q=None, max_q=None, max_le
     if max_len is None:
         max_len = min(width * cache.page_tokens, 2 ** 30)
     if O is None:
-        O, ldo = Q.new_empty((T, hq, d)), hq * d
+        O, ldo = _empty(Q, (T, hq, d), Q.dtype, stream), hq * d
     else:
         _want(O.shape == Q.shape and O.dtype == Q.dtype and O.get_device() == dev, "O: Q's shape, type and device expected")
         ldo = _heads(O, "O", d)
     if work is None:
         nbytes = attention_kv4_workspace_bytes(cache, T, hq, n, max_q, max_len)
-        if nbytes and stream is None:
-            work = torch.empty((nbytes,), dtype=torch.uint8, device=Q.device)
-        elif nbytes:
-            # (Of the call's stream, so that its memory is not handed out on another one while the call waits.)
-            with torch.cuda.stream(stream):
-                work = torch.empty((nbytes,), dtype=torch.uint8, device=Q.device)
+        work = _empty(Q, (nbytes,), torch.uint8, stream) if nbytes else None
     else:
         _want(work.get_device() == dev and work.is_contiguous() and work.element_size() == 1, "work: contiguous bytes on Q's device expected")
     _check(_lib.load().oq_attention_kv4(cache.ref, _ptr(Q), T, ldq, hq, _DTYPE[Q.dtype], _ptr(cu_q), max_q, _ptr(block_table),

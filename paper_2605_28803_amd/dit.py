@@ -270,9 +270,9 @@ class DiT:
 
     def in_projection(self, x, resid=None, stream=None):
         """resid fp32 [M, D] = x W_in^T + b_in for the state x (fp32 [B, S, A])."""
-        from . import _check
+        from . import _check, _empty
         if resid is None:
-            resid = torch.empty((self.M, self.cfg_c.hidden), dtype=torch.float32, device=self.device)
+            resid = _empty(x, (self.M, self.cfg_c.hidden), torch.float32, stream)
         _check(self.lib.oq_dit_in_projection(self.handle, x.data_ptr(), resid.data_ptr(), self._stream(stream)),
                "oq_dit_in_projection")
         return resid
