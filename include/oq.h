@@ -558,7 +558,8 @@ int oq_quantize_weights_step(const void* W_u, int64_t N, int64_t K, int64_t ldw,
 /*
  * A row is one token and kv head, head_dim channels x.  Its codes are q =
  * clamp(round_half_even(7 x / max|x|), -7, 7) (formed exactly: a quotient on a
- * half integer rounds to even, none beside one goes the wrong way), its step
+ * half integer rounds to even, none beside one goes the wrong way; but in rotated bf16
+ * rows whose nonzero elements span more than 2^34 one within 2^-42 of it may), its step
  * fp32 Delta = max|x| / 7, and the value it stands for q Delta; a row of
  * zeros has zero codes and step 0.  With rotate_k the keys are rotated first,
  * x = k H_d / sqrt(d) (d = head_dim, one Hadamard block per head); attention

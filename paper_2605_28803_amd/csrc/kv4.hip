@@ -119,9 +119,12 @@ __device__ __forceinline__ T top_row(const T (&x)[8]) {
 
 // Code of one element: the integer nearest to 7 u / top, ties to even, |u| <=
 // top.  7 u, q top and their difference are exact (u and top are inputs of at
-// most 11 bits, or sums of up to 256 of them in fp64), so a quotient next to
+// most 11 bits, or sums of up to 256 of them in fp64: fp16's need 51 bits, bf16's
+// as many as their exponents span and 19), so a quotient next to
 // a half integer is decided exactly: the estimate is at most one off, and only
-// beside a boundary.
+// beside a boundary.  In rotated bf16 rows whose nonzero elements span more than 2^34 the sums round
+// (by up to 2^-46 of the largest: eight stages, and the sum of magnitudes at most 16 times the norm), and a
+// quotient within 2^-42 of a half integer may go either way.
 template <typename T>
 __device__ __forceinline__ float exact_code(T u, T top) {
   const T q = rint(u * (T(7) / top));
@@ -158,7 +161,7 @@ __device__ __forceinline__ uint32_t codes8(const T (&u)[8], T top) {
 //
 // A workgroup takes the keys and the values of 2048 / d tokens and one head, d / 8
 // lanes a row, both loads in flight from the start.  Rotated keys are summed in
-// fp64, where sums of inputs are exact; that is 8 us of the 30 that 16000 tokens
+// fp64, where sums of inputs are exact (exact_code); that is 8 us of the 30 that 16000 tokens
 // of 8 heads of 128 take (83 MB, 2.8 TB/s; unrotated 22 us, 3.8 TB/s), the rest of
 // it the vector work of max and codes beside the loads.  Codes of values go through LDS, so that a wave stores 16
 // tokens of a channel pair as neighbouring bytes: tokens of a prompt fill their
