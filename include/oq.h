@@ -642,9 +642,11 @@ int oq_kv4_gather(const oq_kv4_cache* cache, const int64_t* slots, int64_t n, vo
  *          calls that share it must not overlap
  * n_seqs n_kv_heads <= 65535, n_heads <= 65535, max_q n_heads / n_kv_heads <= 2^26.
  * Keys, steps and values past a sequence's end are not used, whatever they hold.
- * Queries are used as fp16 times a power of two (rotated ones as two such parts),
- * probabilities as fp16 relative to the largest contribution (a probability times a step;
- * normal numbers down to 2^-29 of it, but not below 2^-140), sums and statistics in fp32.
+ * Queries are used as fp16 times a power of two (rotated ones as two such parts). A score's
+ * fp32 sum starts at 72 sum(q) in units of the key's step, so its rounding is relative to 80
+ * sum |q| of them; scores are finite in fp32. Probabilities are used as fp16 relative to the
+ * largest contribution (a probability times a step; normal numbers down to 2^-29 of it, but
+ * not below 2^-140), sums and statistics in fp32.
  * Errors: OQ_ERR_NULL, OQ_ERR_SHAPE, OQ_ERR_ALIGN, OQ_ERR_ARG,
  * OQ_ERR_WORKSPACE, OQ_ERR_DEVICE, OQ_ERR_HIP.
  */

@@ -17,8 +17,8 @@
 // cycles of matrix instructions, about 700 of the vector unit (32 exponentials at a
 // quarter of its rate, as many multiply-adds, half as many maxima, packed roundings and dot
 // products that add the rounded probabilities) and 32 KB of LDS reads; two waves a SIMD
-// overlap them.  One causal sequence of 8192, 32 / 8 heads of 128: 544 us, 1010
-// TFLOP/s, 85% of what the library's 8192-cubed bf16 product reaches on the same card; 64 rows
+// overlap them.  One causal sequence of 8192, 32 / 8 heads of 128: 537 to 598 us on several cards, 1024 to 920
+// TFLOP/s, about 85% of what the library's 8192-cubed bf16 product reaches; 64 rows
 // a wave (half the LDS reads, one wave a SIMD) 857 against 561 us; 32-key steps 604.
 //
 // Probabilities are rounded to the inputs' type for the second product and
@@ -307,8 +307,9 @@ __global__ __launch_bounds__(64 * RW * KG, 2) void prompt_attn_kernel(PromptArgs
         }
         pf[u][j] = __builtin_bit_cast(v8, pk);
       }
-    // The second product goes before another wave's softmax (1 x 4096, 16 full heads of 128: 143 -> 135 us;
-    // of 256 269 -> 264; at d = 64, and at 128 with key groups, in step at their barrier, up to 1% slower).
+    // The second product goes before another wave's softmax (1 x 4096, 16 full heads of 128: 144 -> 139 us;
+    // of 256 270 -> 268; 32 / 8 causal ones of 128 150 -> 144; at d = 64, and at 128 with key groups, in step at their
+    // barrier, up to 1% slower).
     if constexpr (D == 256 || (KG == 1 && D == 128)) __builtin_amdgcn_s_setprio(1);
 #pragma unroll
     for (int ct = 0; ct < CT; ++ct)
