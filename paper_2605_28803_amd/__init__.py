@@ -50,7 +50,9 @@ def _stream(stream=None):
 
 
 def _on(stream, dev):
-    """_stream on a device that is known to be the current one."""
+    """_stream on a device that is known to be the current one and the tensors'."""
+    if stream is not None and stream.device_index != dev:
+        raise ValueError(f"the stream is not on cuda:{dev}")
     return _raw_stream(dev) if stream is None and _raw_stream is not None else _stream(stream)
 
 
