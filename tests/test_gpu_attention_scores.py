@@ -78,3 +78,14 @@ def test_rows_beside_a_growing_maximum(dtype, d):
     q[::16, 0, 1] = 1.0
     k[:, 0, 1] = torch.arange(n).to(dtype) / 64
     _check(q, k, v, False, scale=1.0)
+
+
+@pytest.mark.parametrize("causal", [True, False])
+@pytest.mark.parametrize("dtype,at", [(torch.float16, 25000.0), (torch.bfloat16, -2.0 ** 40)])
+@pytest.mark.parametrize("n,hq,hk,d", [(100, 3, 1, 64), (100, 3, 1, 128), (100, 3, 1, 256), (700, 52, 4, 128)])
+def test_equal_large_scores_without_key_groups(n, hq, hk, d, dtype, at, causal):
+    # (at most 2 at: 50000 is finite in fp16)
+    q = (at * (1 + torch.arange(n)[:, None, None] / n)).expand(n, hq, d).to(dtype).contiguous()
+    assert torch.isfinite(q).all()
+    v = torch.randn((n, hk, d), generator=torch.Generator().manual_seed(n + d)).to(dtype)
+    _check(q, _keys(n, hk, d, at, at / 2, dtype), v, causal)
