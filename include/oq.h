@@ -413,6 +413,120 @@ int oq_w8a8_gemm_i32(const int8_t* Xq8, int64_t M, const int8_t* Wq8, int64_t N,
                      int32_t* acc, int64_t ldc, void* stream);
 
 /* ------------------------------------------------------------------------ */
+/* Linears in microscaled 4-bit floating point, and what stands between them  */
+/* ------------------------------------------------------------------------ */
+/*
+ * MX4 codes: blocks of 32 channels of a row share a step 2^s, s =
+ * floor(log2 max|y|) - 2 clamped to [-127, 127] (0: -127); a channel's code is y /
+ * 2^s rounded to the nearest of 0, 1/2, 1, 3/2, 2, 3, 4, 6 (ties to the even
+ * code, past 6: 6), its index in bits 0 .. 2 and the sign in bit 3.  Unlike the
+ * int4 codes above they need no step per token and channel in an epilogue: the
+ * matrix cores take the steps.
+ *   codes  uint8 [rows][K / 2], the even channel in the low nibble;
+ *   steps  uint8 [rows][oq_mx4_step_bytes(K)], byte b of a row s + 127 of its
+ *          channels 32 b .. 32 b + 31, 255: an infinity or a NaN among them (its
+ *          codes are 0 and its values NaN).  The bytes of a row past K / 32 are
+ *          neither written nor used.
+ * K % 32 == 0, 32 <= K <= OQ_MX4_MAX_K; codes and steps 16-byte aligned.
+ * The producers' codes are those of their formulas in 64 bits; a ratio within
+ * about 2^-45 of a border between two codes may go either way.
+ */
+#define OQ_MX4_MAX_K 65536
+
+/* Bytes from one row's steps to the next: 16 ceil(K / 512). */
+size_t oq_mx4_step_bytes(int64_t K);
+
+/*
+ * oq_mx4_quantize -- codes and steps of rows of activations or weights, rotated
+ * first if wanted: y = x . blockdiag(H_b) / sqrt(b) in blocks of b = had_block
+ * channels (as oq_rotate_quantize_act; the two operands of a product need the
+ * same b).
+ * X         device fp16 or bf16 (dtype) [M][ldx], ldx >= K, % 8 == 0, 16-byte aligned
+ * had_block 1 (none), 32, 64 or 128, dividing K
+ * Xq, steps device, as above; may not overlap X
+ * Errors: OQ_ERR_NULL, OQ_ERR_SHAPE, OQ_ERR_ALIGN, OQ_ERR_ARG, OQ_ERR_DEVICE,
+ * OQ_ERR_HIP.
+ */
+int oq_mx4_quantize(const void* X, int64_t M, int64_t K, int64_t ldx, int32_t dtype, int32_t had_block,
+                    uint8_t* Xq, uint8_t* steps, void* stream);
+
+/*
+ * oq_mx4_dequantize -- the values of rows of codes, X device [M][ldx] of
+ * out_dtype (fp16, bf16, fp32; ldx >= K, % 8 == 0, 16-byte aligned).  fp32 and
+ * bf16 hold every value but 3, 4 and 6 times 2^127 (infinite); fp16 rounds.
+ * A rotation is not undone.  Errors as oq_mx4_quantize.
+ */
+int oq_mx4_dequantize(const uint8_t* Xq, const uint8_t* steps, int64_t M, int64_t K, void* X, int64_t ldx,
+                      int32_t out_dtype, void* stream);
+
+/*
+ * oq_mx4_linear -- Y[i][n] = round_to_out(sum_k x[i][k] w[n][k] + bias[n]), x and
+ * w the values of the codes, products exact and sums in fp32.
+ * Xq, x_steps  device, [M] rows of K codes;  Wq, w_steps  device, [N] rows
+ * bias         device fp16 [N] or NULL
+ * M >= 0, N >= 1
+ * Y            device [M][ldy] of out_dtype (fp16, bf16, fp32), ldy >= N, % 8 == 0,
+ *              16-byte aligned; may not overlap the operands
+ * A block with byte 255 makes its row's (column's) outputs NaN, no others.
+ * Errors as oq_mx4_quantize.
+ */
+int oq_mx4_linear(const uint8_t* Xq, const uint8_t* x_steps, int64_t M, const uint8_t* Wq, const uint8_t* w_steps,
+                  const void* bias, int64_t N, int64_t K, void* Y, int64_t ldy, int32_t out_dtype, void* stream);
+
+/*
+ * oq_gated_activation -- h = act(g) u of rows [g | u] as a gate|up linear writes
+ * them, act(g) = g / (1 + e^-t), t = g (SiLU) or 2 sqrt(2 / pi) (g + 0.044715 g^3)
+ * (GELU in its tanh form), in 16 bits or as the codes of the next linear.
+ * GU       device fp16 or bf16 (dtype) [M][ld], g in columns 0 .. F - 1, u in F ..
+ *          2 F - 1; ld >= 2 F, % 8 == 0, 16-byte aligned
+ * F        % 8 == 0 (codes: % 32), 8 <= F <= OQ_MX4_MAX_K
+ * H        device [M][ldh] of dtype (ldh >= F, % 8 == 0, 16-byte aligned), or NULL
+ *          and Hq, steps: device codes of h (not rounded to dtype first)
+ * Outputs may not overlap GU.  Errors as oq_mx4_quantize (OQ_ERR_ARG: act, both outputs).
+ */
+typedef enum { OQ_ACT_GELU_TANH = 0, OQ_ACT_SILU = 1 } oq_act;
+int oq_gated_activation(const void* GU, int64_t M, int64_t F, int64_t ld, int32_t dtype, int32_t act, void* H,
+                        int64_t ldh, uint8_t* Hq, uint8_t* steps, void* stream);
+
+/*
+ * oq_residual_norm -- the residual stream between two blocks, in one pass:
+ *   r' = alpha R + gate[g] * post(Y),   h = pre(r') * (1 + scale[g]) + shift[g]
+ * with post and pre each none, RMSNorm x / sqrt(mean(x^2) + eps) * gain + bias or
+ * LayerNorm (x - mean) / sqrt(var + eps) * gain + bias (var of D values), and h
+ * formed from the unrounded r'.
+ * R        device [M][ldr] of r_dtype (fp32, or dtype), or NULL: 0
+ * Y        device [M][ldy] of dtype (fp16 or bf16), the block's output, or NULL: 0
+ * post     host, or NULL: none (y as it is)
+ * pre      host, or NULL: none (no h)
+ * gate, scale, shift  device [n_mod][ld_mod] of dtype, each may be NULL (1, 0, 0);
+ *          ld_mod >= D, % 8 == 0 (so that they may be parts of one modulation row)
+ * mod_row  device int32 [M]: row of these for each token (out of range: the
+ *          token's outputs are left as they were), or NULL: row 0
+ * R_out    device [M][ldro] of r_dtype, may be R (with ldro = ldr), or NULL: not wanted
+ * H        device [M][ldh] of dtype, may be Y (with ldh = ldy), or NULL and Hq,
+ *          steps: device MX4 codes of h (not rounded to dtype first)
+ * D % 8 == 0 (codes: % 32), 8 <= D <= OQ_NORM_MAX_D; strides >= D, % 8 == 0; alpha
+ * finite; pointers 16-byte aligned.  Other overlaps of outputs are not allowed.
+ * Sums are fp32 over at most 32 values of a thread and fp64 beyond; with codes all fp64.
+ * Errors: as oq_mx4_quantize (OQ_ERR_ARG: kind, eps, alpha, h without pre, both
+ * outputs; OQ_ERR_NULL: neither R nor Y, or no output).
+ */
+#define OQ_NORM_MAX_D 16384
+typedef enum { OQ_NORM_NONE = 0, OQ_NORM_RMS = 1, OQ_NORM_LAYER = 2 } oq_norm_kind;
+typedef struct {
+  int32_t kind;      /* oq_norm_kind */
+  float eps;         /* > 0, <= 1 */
+  float gain_offset; /* the gain is gain_offset + gain (1 for gains stored about 0) */
+  const void* gain;  /* device [D] of dtype, 16-byte aligned, or NULL: 1 */
+  const void* bias;  /* device [D] of dtype, 16-byte aligned, or NULL: 0 */
+} oq_norm;
+int oq_residual_norm(const void* R, int64_t ldr, int32_t r_dtype, const void* Y, int64_t ldy, int32_t dtype,
+                     int64_t M, int64_t D, const oq_norm* post, const oq_norm* pre, float alpha,
+                     const void* gate, const void* scale, const void* shift, int64_t ld_mod, int64_t n_mod,
+                     const int32_t* mod_row, void* R_out, int64_t ldro, void* H, int64_t ldh, uint8_t* Hq,
+                     uint8_t* steps, void* stream);
+
+/* ------------------------------------------------------------------------ */
 /* Attention over packed prompts                                             */
 /* ------------------------------------------------------------------------ */
 /*

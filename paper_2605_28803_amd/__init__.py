@@ -524,4 +524,6 @@ def quantize_weights_step_host(W_u: np.ndarray, had_block: int, delta: np.ndarra
 
 from .attention import (KV4Cache, attention_kv4, attention_kv4_workspace_bytes, attention_prompt,  # noqa: E402,F401
                         kv4_append, kv4_gather)
+from .mx4 import (ACT_GELU_TANH, ACT_SILU, Norm, gated_activation, mx4_dequantize, mx4_linear,  # noqa: E402,F401
+                  mx4_quantize, mx4_step_bytes, residual_norm)
 from .dit import DiT  # noqa: E402,F401

@@ -40,6 +40,10 @@ class oq_kv4_cache(C.Structure):
                 ("page_tokens", i32), ("n_kv_heads", i32), ("head_dim", i32), ("rotate_k", i32)]
 
 
+class oq_norm(C.Structure):
+    _fields_ = [("kind", i32), ("eps", C.c_float), ("gain_offset", C.c_float), ("gain", vp), ("bias", vp)]
+
+
 # name -> (restype, argtypes)
 SIGNATURES = {
     "oq_status_string": (C.c_char_p, [i32]),
@@ -78,6 +82,13 @@ SIGNATURES = {
     "oq_quantize_weights_i8": (i32, [vp, i64, i64, i64, i32, vp, vp, vp]),
     "oq_w8a8_linear": (i32, [vp, vp, i64, vp, vp, vp, i64, i64, vp, i64, i32, vp]),
     "oq_w8a8_gemm_i32": (i32, [vp, i64, vp, i64, i64, vp, i64, vp]),
+    "oq_mx4_step_bytes": (C.c_size_t, [i64]),
+    "oq_mx4_quantize": (i32, [vp, i64, i64, i64, i32, i32, vp, vp, vp]),
+    "oq_mx4_dequantize": (i32, [vp, vp, i64, i64, vp, i64, i32, vp]),
+    "oq_mx4_linear": (i32, [vp, vp, i64, vp, vp, vp, i64, i64, vp, i64, i32, vp]),
+    "oq_gated_activation": (i32, [vp, i64, i64, i64, i32, i32, vp, i64, vp, vp, vp]),
+    "oq_residual_norm": (i32, [vp, i64, i32, vp, i64, i32, i64, i64, C.POINTER(oq_norm), C.POINTER(oq_norm), C.c_float,
+                               vp, vp, vp, i64, i64, vp, vp, i64, vp, i64, vp, vp, vp]),
     "oq_attention_prompt": (i32, [vp, vp, vp, i64, i64, i64, i64, i32, vp, i32, i32, i32, i32, i32, C.c_float, vp, i64,
                                   vp]),
     "oq_kv4_append": (i32, [C.POINTER(oq_kv4_cache), vp, vp, i64, i64, i64, i32, vp, vp]),
