@@ -197,4 +197,66 @@ constexpr W8Split w8_split(int64_t M, int64_t N, int64_t K) {
   return s;
 }
 
+// Microscaled 4-bit product: estimated us of the weight-streaming kernel (one row
+// block of 16 and 16 columns a workgroup; each reads its rows and columns at what the
+// level-two caches give) and of the ring's tilings, and the fastest of them.
+// Over 100 shapes from 24 x 1024 x 1024 to 4096 x 8192 x 8192 the one chosen takes 1.4% longer than the fastest
+// in the mean (the host test holds them).
+//   256 x 256 tiles of 8 waves of 128 x 64, two buffers;  128 x 128 of 8 waves, four
+//   buffers, for one tile a CU, or of 4 waves, two buffers and two workgroups a CU;
+//   64 x 64 of 4 waves and 128 x 64, four buffers.
+constexpr int kTilingsMx4 = 5;
+constexpr RingCost kRingCostMx4[kTilingsMx4] = {{256, 256, 1, 5.7f, 7.5f, 5.5f},
+                                                {128, 128, 1, 2.15f, 2.9f, 3.7f},
+                                                {128, 128, 2, 3.6f, 2.6f, 4.2f},
+                                                {64, 64, 2, 1.07f, 1.2f, 2.9f},
+                                                {128, 64, 1, 1.45f, 1.77f, 3.6f}};
+constexpr float mx4_estimate(const RingCost& c, int64_t M, int64_t N, int64_t K) {
+  const int64_t tiles = ((M + c.bm - 1) / c.bm) * ((N + c.bn - 1) / c.bn);
+  const int64_t n = (tiles + 255) / 256, rounds = (n + c.occ - 1) / c.occ;
+  // (One tile a CU: slower the more of the chip is at work.)
+  const float fill = c.lat + (c.thr - c.lat) * static_cast<float>(tiles) / 256.0f;
+  const float per = n > 1 ? static_cast<float>(n) * c.thr : fill;
+  const float k = 2.0f * static_cast<float>(rounds - 1) + 1e-3f * static_cast<float>(K) * (per > c.lat ? per : c.lat);
+  const float hbm = (static_cast<float>(M + N) * static_cast<float>(K) * 0.53f + 2.0f * static_cast<float>(M) * static_cast<float>(N)) / 4.8e6f;
+  return c.fixed + (k > hbm ? k : hbm);
+}
+constexpr float mx4_small_estimate(int64_t M, int64_t N, int64_t K) {
+  const float groups = static_cast<float>((N + 15) / 16) * static_cast<float>((M + 15) / 16), k = static_cast<float>(K);
+  const float wait = 1.9f + 0.55e-3f * k * (M == 1 ? 0.7f : 1.0f);
+  const float read = 0.8f + 0.8e-3f * groups + groups * static_cast<float>(16 + (M < 16 ? M : 16)) * k * 0.53f / 6.8e6f;
+  return wait > read ? wait : read;
+}
+constexpr int mx4_tiling(int64_t M, int64_t N, int64_t K) {
+  int best = 0;
+  for (int i = 1; i < kTilingsMx4; ++i)
+    if (mx4_estimate(kRingCostMx4[i], M, N, K) < mx4_estimate(kRingCostMx4[best], M, N, K)) best = i;
+  return best;
+}
+constexpr bool mx4_few_rows(int64_t M, int64_t N, int64_t K) {
+  return M <= 256 && mx4_small_estimate(M, N, K) < mx4_estimate(kRingCostMx4[mx4_tiling(M, N, K)], M, N, K);
+}
+// Waves of a workgroup of the weight-streaming kernel: one or two units of 512 codes each up to K = 16384.  Us
+// of 4 / 8 / 16: 1 x 2560 x 2048 2.8 / 2.8 / 2.9, 1 x 4096 x 4096 4.7 / 4.3 / 4.4, 1 x 2048 x 16384 11.0 / 9.4 / 8.7,
+// 1 x 32768 x 2048 8.9 / 9.0 / 12.4.
+constexpr int mx4_small_waves(int64_t K) { return K <= 2048 ? 4 : K <= 4096 ? 8 : 16; }
+constexpr float mx4_best(int64_t M, int64_t N, int64_t K) {
+  const float ring = mx4_estimate(kRingCostMx4[mx4_tiling(M, N, K)], M, N, K);
+  return mx4_few_rows(M, N, K) ? mx4_small_estimate(M, N, K) : ring;
+}
+// As w8_split: the whole rounds of 256 x 256 tiles, and the rest on what suits it.
+constexpr W8Split mx4_split(int64_t M, int64_t N, int64_t K) {
+  W8Split s{true, 0};
+  const int64_t tm = (M + 255) / 256, tn = (N + 255) / 256, rounds = tm * tn / 256;
+  if (rounds < 1) return s;
+  float best = 0.92f * mx4_best(M, N, K);
+  const int64_t n1 = rounds * 256 / tm * 256, m1 = rounds * 256 / tn * 256;
+  if (n1 > 0 && n1 < N && mx4_tiling(M, n1, K) == 0 && mx4_best(M, n1, K) + mx4_best(M, N - n1, K) < best) {
+    best = mx4_best(M, n1, K) + mx4_best(M, N - n1, K);
+    s = W8Split{true, n1};
+  }
+  if (m1 > 0 && m1 < M && mx4_tiling(m1, N, K) == 0 && mx4_best(m1, N, K) + mx4_best(M - m1, N, K) < best) s = W8Split{false, m1};
+  return s;
+}
+
 }  // namespace oq

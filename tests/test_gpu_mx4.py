@@ -104,6 +104,11 @@ SHAPES = [(1, 1, 32), (1, 16, 64), (1, 2560, 2048), (2, 24, 512), (3, 17, 96), (
           (200, 1000, 2080), (256, 512, 16384), (257, 129, 32), (300, 2049, 1536), (512, 768, 256), (700, 800, 1024), (8, 72, 65536)]
 
 
+# Enough rows and columns for the large tiles, alone and with a rest in a launch of its own.
+LARGE = [(2100, 8200, 1056), (8000, 2050, 1056), (4100, 2050, 544), (4100, 2050, 4160), (200, 8200, 4160), (4100, 1000, 544),
+         (4100, 1000, 4160), (65, 8200, 4160), (65, 8200, 1056), (200, 8200, 96)]
+
+
 @pytest.mark.parametrize("M,N,K", SHAPES)
 @pytest.mark.parametrize("out", [torch.float16, torch.bfloat16, torch.float32])
 def test_linear(M, N, K, out):
@@ -119,7 +124,19 @@ def test_linear(M, N, K, out):
     assert again.shape == (M, N) and torch.equal(again, Y[:M, :N])  # (the steps' unused bytes do not matter)
 
 
-@pytest.mark.parametrize("M,N,K", [(3, 40, 1024), (130, 300, 544), (600, 520, 2048)])
+@pytest.mark.parametrize("M,N,K", LARGE)
+def test_linear_large(M, N, K):
+    xi, xb, wi, wb = operands(M, N, K, M + N + K)
+    bias = torch.randn((N,), generator=torch.Generator().manual_seed(N)).half() if M % 20 else None
+    want, bound = R.linear(xi, xb, wi, wb, bias)
+    for out in (torch.float16, torch.float32) if M % 20 else (torch.bfloat16,):
+        Y = torch.full((M + 1, (N + 7) // 8 * 8 + 8), 77.0, dtype=out, device=DEV)
+        oq.mx4_linear(*R.pack(xi, xb, DEV), *R.pack(wi, wb, DEV), None if bias is None else bias.to(DEV), OUT[out], Y[:M, :N])
+        R.check(Y[:M, :N], want, bound, out)
+        assert bool((Y[M] == 77).all()) and bool((Y[:, N:] == 77).all())
+
+
+@pytest.mark.parametrize("M,N,K", [(3, 40, 1024), (130, 300, 544), (600, 520, 2048), (4100, 2050, 544), (4100, 2050, 2080)])
 def test_linear_where_each_block_goes(M, N, K):
     """Blocks of one operand that are 1 in a single channel: the product reads the
     other operand's channel, whatever block order the kernel has inside."""
