@@ -64,57 +64,113 @@ __global__ __launch_bounds__(kThreads) void mx4_quantize_kernel(QuantArgs a) {
 }
 
 // Rotated in blocks of 2^LOG channels (5, 6, 7): a thread takes a block of 32,
-// whose five stages are its own; the others exchange with the lanes 1 and 2
-// away.  In double the sums of fp16 values are exact.
+// whose five stages are its own; the others exchange with the lanes 1 and 2 away.
+//
+// The stages run in float.  A sum of 2^LOG inputs is then off by at most LOG 2^-24
+// sum|x|, and twice a rounding more follow, so codes that the two ends of that
+// interval share are the exact ones'; a wave that holds another (1 in 50 for
+// blocks of 32, 1 in 15 for 128) repeats its blocks in double, where the sums of
+// fp16 values are exact.  Double for all of them costs twice the operations
+// (16384 x 4096 in blocks of 128: 57 us).
+template <int LOG, typename F>
+__device__ __forceinline__ void hadamard32(F (&v)[32]) {
+#pragma unroll
+  for (int h = 1; h < 32; h *= 2)
+#pragma unroll
+    for (int e = 0; e < 32; ++e)
+      if (!(e & h)) {
+        const F x = v[e], y = v[e + h];
+        v[e] = x + y;
+        v[e + h] = x - y;
+      }
+  auto exchange = [&](auto CTRL, bool upper) {
+    constexpr int c = decltype(CTRL)::value;
+    const F sign = upper ? static_cast<F>(-1) : static_cast<F>(1);
+#pragma unroll
+    for (int e = 0; e < 32; ++e) {
+      if constexpr (sizeof(F) == 8) {
+        const uint64_t b = __builtin_bit_cast(uint64_t, v[e]);
+        const uint64_t o = static_cast<uint64_t>(dpp<c>(static_cast<uint32_t>(b >> 32))) << 32 | dpp<c>(static_cast<uint32_t>(b));
+        v[e] = fma(sign, v[e], __builtin_bit_cast(F, o));
+      } else {
+        v[e] = fmaf(sign, v[e], __uint_as_float(dpp<c>(__float_as_uint(v[e]))));
+      }
+    }
+  };
+  if constexpr (LOG >= 6) exchange(std::integral_constant<int, kQuadXor1>{}, threadIdx.x & 1);
+  if constexpr (LOG >= 7) exchange(std::integral_constant<int, kQuadXor2>{}, threadIdx.x & 2);
+}
+
 template <bool BF, int LOG>
 __global__ __launch_bounds__(kThreads) void mx4_rotate_quantize_kernel(QuantArgs a) {
   const uint32_t i = blockIdx.x * kThreads + threadIdx.x;
   if (i >= a.pieces) return;  // (pieces of 32 here; whole rotation blocks)
   const uint32_t r = divide(i, a.row), p = i - r * a.row.d;
   const uint4* src = reinterpret_cast<const uint4*>(a.X + r * a.ldx + p * 32);
-  double v[32];
+  constexpr double norm = LOG == 5 ? 0.17677669529663688110 : LOG == 6 ? 0.125 : 0.08838834764831844055;
+  uint32_t c[4], byte;
+  bool open;
+  {
+    float v[32], sum = 0.0f;
 #pragma unroll
-  for (int c = 0; c < 4; ++c) {
-    const uint4 q = src[c];
+    for (int g = 0; g < 4; ++g) {
+      const uint4 q = src[g];
 #pragma unroll
-    for (int e = 0; e < 8; ++e) v[8 * c + e] = static_cast<double>(half8<BF>(q, e));
-  }
-#pragma unroll
-  for (int h = 1; h < 32; h *= 2)
-#pragma unroll
-    for (int e = 0; e < 32; ++e)
-      if (!(e & h)) {
-        const double x = v[e], y = v[e + h];
-        v[e] = x + y;
-        v[e + h] = x - y;
+      for (int e = 0; e < 8; ++e) {
+        v[8 * g + e] = half8<BF>(q, e);
+        sum += fabsf(v[8 * g + e]);
       }
-  auto exchange = [&](auto CTRL, bool upper) {
-    const double sign = upper ? -1.0 : 1.0;
+    }
+    if constexpr (LOG >= 6) sum += __uint_as_float(dpp<kQuadXor1>(__float_as_uint(sum)));
+    if constexpr (LOG >= 7) sum += __uint_as_float(dpp<kQuadXor2>(__float_as_uint(sum)));
+    hadamard32<LOG>(v);
+    float top = 0.0f;
 #pragma unroll
     for (int e = 0; e < 32; ++e) {
-      const uint64_t b = __builtin_bit_cast(uint64_t, v[e]);
-      const uint64_t o = static_cast<uint64_t>(dpp<decltype(CTRL)::value>(static_cast<uint32_t>(b >> 32))) << 32 |
-                         dpp<decltype(CTRL)::value>(static_cast<uint32_t>(b));
-      v[e] = fma(sign, v[e], __builtin_bit_cast(double, o));
+      v[e] *= static_cast<float>(norm);
+      top = fmaxf(top, fabsf(v[e]));
     }
-  };
-  if constexpr (LOG >= 6) exchange(std::integral_constant<int, kQuadXor1>{}, threadIdx.x & 1);
-  if constexpr (LOG >= 7) exchange(std::integral_constant<int, kQuadXor2>{}, threadIdx.x & 2);
-  constexpr double norm = LOG == 5 ? 0.17677669529663688110 : LOG == 6 ? 0.125 : 0.08838834764831844055;
-  uint32_t top = 0;
+    const float off = sum * static_cast<float>(norm) * ((LOG + 4) * 0x1p-24f);  // (the sum's and the product's own roundings too)
+    const uint32_t th = __float_as_uint(top + off), tl = __float_as_uint(top - off);
+    byte = step_byte(th >> 23);
+    const float step = step_of(byte);
+    // Undecided: the step, a code, or a block outside the range in which floats are this near.  (A block of zeros is decided.)
+    open = (th ^ tl) >> 23 != 0 || !(sum < 0x1p100f) || (sum < 0x1p-90f && sum != 0.0f);
 #pragma unroll
-  for (int e = 0; e < 32; ++e) {
-    v[e] *= norm;
-    top = max(top, high_word(v[e]));
+    for (int g = 0; g < 4; ++g) {
+      float up[8], down[8];
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        up[e] = v[8 * g + e] + off;
+        down[e] = v[8 * g + e] - off;
+      }
+      c[g] = codes8(up, step);
+      open |= c[g] != codes8(down, step);
+    }
   }
-  const uint32_t byte = step_byte64(top);
-  uint32_t c[4];
+  if (__any(open)) {
+    double v[32];
 #pragma unroll
-  for (int g = 0; g < 4; ++g) {
-    double w[8];
+    for (int g = 0; g < 4; ++g) {
+      const uint4 q = src[g];
 #pragma unroll
-    for (int e = 0; e < 8; ++e) w[e] = v[8 * g + e];
-    c[g] = codes8(w, byte);
+      for (int e = 0; e < 8; ++e) v[8 * g + e] = static_cast<double>(half8<BF>(q, e));
+    }
+    hadamard32<LOG>(v);
+    uint32_t top = 0;
+#pragma unroll
+    for (int e = 0; e < 32; ++e) {
+      v[e] *= norm;
+      top = max(top, high_word(v[e]));
+    }
+    byte = step_byte64(top);
+#pragma unroll
+    for (int g = 0; g < 4; ++g) {
+      double w[8];
+#pragma unroll
+      for (int e = 0; e < 8; ++e) w[e] = v[8 * g + e];
+      c[g] = codes8(w, byte);
+    }
   }
   reinterpret_cast<uint4*>(a.Xq)[i] = make_uint4(c[0], c[1], c[2], c[3]);
   a.steps[r * a.lds + p] = static_cast<uint8_t>(byte);

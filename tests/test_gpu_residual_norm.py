@@ -138,6 +138,29 @@ def test_rows_without_a_modulation(mx4, M, D):
         assert bool((h.cpu()[~keep] == 6).all())
 
 
+@pytest.mark.parametrize("mx4", [False, True])
+@pytest.mark.parametrize("M,D,rt", [(17000, 32, B), (9000, 64, F32), (4500, 1024, F32), (4500, 1024, B), (4200, 2048, B), (2100, 4096, F32), (1100, 8192, F32),
+                                    (1100, 16384, B), (1100, 16384, F32)])
+def test_more_rows_than_the_chip_holds(mx4, M, D, rt):
+    """A workgroup's second and third row are worked on as its first, also behind one
+    that is skipped."""
+    t = make(M, D, B, rt, D, 3)
+    p, q, rp, rq = norms(t, "layer", "rms")
+    t["row"][::5] = -1
+    keep = t["row"] >= 0
+    out = torch.full((M, D), 5.0, dtype=rt, device=DEV)
+    r, h = oq.residual_norm(t["R"].to(DEV), t["Y"].to(DEV), p, q, 1.5, t["gate"].to(DEV), t["scale"].to(DEV), t["shift"].to(DEV), t["row"].to(DEV), mx4, out)
+    assert bool((r[~keep.to(DEV)] == 5).all())
+    for n in ("R", "Y", "row"):
+        t[n] = t[n][keep]
+    wr, er, wh, eh = R.residual_norm(t["R"], t["Y"], rp, rq, 1.5, pick(t, "gate"), pick(t, "scale"), pick(t, "shift"))
+    R.check(r.cpu()[keep], wr, er, rt)
+    if mx4:
+        R.check_codes([c.cpu()[keep] for c in h], wh)
+    else:
+        R.check(h.cpu()[keep], wh, eh, B)
+
+
 @pytest.mark.parametrize("M,D", [(4, 512), (3, 4096), (700, 2048)])
 def test_in_place_is_the_same(M, D):
     t = make(M, D, H, H, 4)
