@@ -102,7 +102,8 @@ __global__ __launch_bounds__(W == 1 ? 256 : 64 * W) void residual_norm_kernel(No
   using Acc = std::conditional_t<MX4, double, float>;
   constexpr int T = 64 * W;  // threads of a row
   constexpr bool AHEAD = !(MX4 && P * W > 16);  // (there the registers do not reach)
-  // (An exchange of a row of its own, rows in turn of two sets: a set is written again behind another row's barriers.)
+  // (An exchange of a row of its own, rows in turn of two sets: a set is written again behind another row's
+  // barriers.  A row that is left has none, and takes no set.)
   __shared__ double red[2][4][W];
   const int tid = W == 1 ? threadIdx.x & 63 : threadIdx.x;
   const bool all = a.D == 8 * T * P;
@@ -148,7 +149,7 @@ __global__ __launch_bounds__(W == 1 ? 256 : 64 * W) void residual_norm_kernel(No
   int64_t row = W == 1 ? static_cast<int64_t>(blockIdx.x) * 4 + (threadIdx.x >> 6) : blockIdx.x;
   if (row >= a.M) return;
   load(row);
-  for (int set = 0;; set ^= 1) {
+  for (int set = 0;;) {
     const int64_t next = row + step;
     int64_t g = 0;
     bool there = true;
@@ -320,6 +321,7 @@ __global__ __launch_bounds__(W == 1 ? 256 : 64 * W) void residual_norm_kernel(No
     }
     if (next >= a.M) return;
     row = next;
+    if (there) set ^= 1;
     if (!AHEAD) load(next);
   }
 }

@@ -161,6 +161,23 @@ def test_more_rows_than_the_chip_holds(mx4, M, D, rt):
         R.check(h.cpu()[keep], wh, eh, B)
 
 
+@pytest.mark.parametrize("mx4", [False, True])
+@pytest.mark.parametrize("M,D,holds", [(5120, 1536, 1024), (2560, 8192, 512)])
+def test_skipped_rows_between_others(mx4, M, D, holds):
+    """One exchange a row, and every other row of a workgroup left: the rows on either
+    side do not share its memory."""
+    t = make(M, D, B, B, D, 2)
+    t["row"] = torch.where(torch.arange(M) // holds % 2 == 1, -1, 0).to(torch.int32)
+    keep = t["row"] >= 0
+    p, _, rp, _ = norms(t, "rms", None)
+    _, h = oq.residual_norm(t["R"].to(DEV), t["Y"].to(DEV), p, None, 1.5, t["gate"].to(DEV), None, None, t["row"].to(DEV), mx4)
+    _, _, wh, eh = R.residual_norm(t["R"][keep], t["Y"][keep], rp, None, 1.5, t["gate"][:1].double().expand(int(keep.sum()), D), None, None)
+    if mx4:
+        R.check_codes([c.cpu()[keep] for c in h], wh)
+    else:
+        R.check(h.cpu()[keep], wh, eh, B)
+
+
 @pytest.mark.parametrize("M,D", [(4, 512), (3, 4096), (700, 2048)])
 def test_in_place_is_the_same(M, D):
     t = make(M, D, H, H, 4)
