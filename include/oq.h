@@ -64,7 +64,8 @@ typedef enum {
 } oq_status;
 
 /* Output element type of the dequantizing epilogue, and element type of the
- * attention and cache operands (OQ_OUT_F32: outputs of oq_kv4_gather only). */
+ * attention and cache operands (OQ_OUT_F32: outputs of oq_kv4_gather and of the
+ * MX4 operators, and residual rows). */
 typedef enum { OQ_OUT_F16 = 0, OQ_OUT_BF16 = 1, OQ_OUT_F32 = 2 } oq_out_dtype;
 
 /* Largest Hadamard block the rotation kernel accepts. */
@@ -501,13 +502,15 @@ int oq_gated_activation(const void* GU, int64_t M, int64_t F, int64_t ld, int32_
  * gate, scale, shift  device [n_mod][ld_mod] of dtype, each may be NULL (1, 0, 0);
  *          ld_mod >= D, % 8 == 0 (so that they may be parts of one modulation row)
  * mod_row  device int32 [M]: row of these for each token (out of range: the
- *          token's outputs are left as they were), or NULL: row 0
+ *          token's outputs are left as they were), or NULL: row 0; without any of
+ *          the three it is not used
  * R_out    device [M][ldro] of r_dtype, may be R (with ldro = ldr), or NULL: not wanted
  * H        device [M][ldh] of dtype, may be Y (with ldh = ldy), or NULL and Hq,
  *          steps: device MX4 codes of h (not rounded to dtype first)
  * D % 8 == 0 (codes: % 32), 8 <= D <= OQ_NORM_MAX_D; strides >= D, % 8 == 0; alpha
  * finite; pointers 16-byte aligned.  Other overlaps of outputs are not allowed.
- * Sums are fp32 over at most 32 values of a thread and fp64 beyond; with codes all fp64.
+ * Sums are fp32 over at most 32 values of a thread and fp64 beyond (finite if the values are
+ * below 2^60 in magnitude); with codes all fp64.
  * Errors: as oq_mx4_quantize (OQ_ERR_ARG: kind, eps, alpha, h without pre, both
  * outputs; OQ_ERR_NULL: neither R nor Y, or no output).
  */

@@ -71,7 +71,7 @@ __global__ __launch_bounds__(kThreads) void mx4_quantize_kernel(QuantArgs a) {
 // interval share are the exact ones'; a wave that holds another (1 in 50 for
 // blocks of 32, 1 in 15 for 128) repeats its blocks in double, where the sums of
 // fp16 values are exact.  Double for all of them costs twice the operations
-// (16384 x 4096 in blocks of 128: 57 us).
+// (16384 x 4096 in blocks of 128: 57 us, so 43).
 template <int LOG, typename F>
 __device__ __forceinline__ void hadamard32(F (&v)[32]) {
 #pragma unroll

@@ -153,7 +153,9 @@ def gated_activation(GU, act=ACT_GELU_TANH, mx4=False, H=None, stream=None):
 
 class Norm:
     """A norm's parameters (oq_norm): kind "rms" or "layer", gain and bias [D]
-    (fp16 or bf16) or None; the gain used is gain_offset + gain."""
+    (fp16 or bf16) or None; the gain used is gain_offset + gain.  It holds the
+    memory that the tensors have now: values written in place are seen, another
+    storage given to them later (module.to(), .data =) needs another Norm."""
 
     KINDS = {"rms": 1, "layer": 2}
 
@@ -163,11 +165,16 @@ class Norm:
         for t in there:
             _want(t.dim() == 1 and t.is_contiguous() and t.dtype in _HALF, "gain, bias: contiguous float16 or bfloat16 [D] expected")
         _want(len({(t.dtype, t.shape, t.device) for t in there}) < 2, "gain and bias need one type, length and device")
-        self.kind, self.gain, self.bias = kind, gain, bias
+        self.kind = kind
+        # (Aliases, so that the memory stays whatever becomes of the tensors.)
+        self._gain, self._bias = (None if t is None else t.detach() for t in (gain, bias))
         # What a call checks: (type, channels, device), or None without parameters.
         self.of = (there[0].dtype, there[0].shape[0], there[0].get_device()) if there else None
         self._c = _lib.oq_norm(self.KINDS[kind], eps, gain_offset, _ptr(gain), _ptr(bias))
         self.ref = C.byref(self._c)
+
+    gain = property(lambda self: self._gain)
+    bias = property(lambda self: self._bias)
 
 
 def residual_norm(R, Y=None, pre=None, post=None, alpha=1.0, gate=None, scale=None, shift=None, mod_row=None, mx4=False,
