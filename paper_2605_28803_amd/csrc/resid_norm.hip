@@ -6,22 +6,19 @@
 //   h  = pre(r') (1 + scale[g]) + shift[g]    (16 bits, or microscaled 4-bit codes)
 //
 // A row's values stay in registers between its sums, so r and y are read once
-// and r' and h written once, and a workgroup takes row after row, the next one's
-// loads under way.  A thread holds P pieces of 8 channels of a row, W waves a row
-// (W = 1: a wave a row, four rows a workgroup, and no barrier).  With an fp32
-// residual a piece is two fours apart, so that every 16-byte access of a wave is
-// of one kilobyte (eight together, 32 bytes a lane: 16384 x 4096 into 16 bits 199
-// us, so 180).
+// and r' and h written once.  A thread holds P pieces of 8 channels of a row, W
+// waves a row (W = 1: four rows a workgroup, and no barrier).  (A workgroup that
+// takes row after row with the next one's loads under way holds more registers
+// and was 3% to 13% slower; pieces of an fp32 residual two fours apart, so that its
+// accesses are of whole kilobytes, cost 4% to 15%.)
 // Sums of a thread's values are float (double where codes are written), sums
 // over threads double.  LayerNorm sums (x - mean)^2 with the mean known: a
 // second exchange, but no cancellation.
 // Where codes are written, everything is double: the codes are then those of the
-// formula in 64 bits, not those of a nearby float.  (Only r' in double and h in
-// float with a bound, undecided codes again in double, held more registers and
-// was no faster.)
-// Bound by memory with 16-bit outputs (16384 x 4096, bf16 residual: 537 MB in 114
-// us, 4.7 TB/s; a copy reaches 5.1), by the double operations and the registers that
-// they hold with codes (fp32 residual: 705 MB in 196 us).
+// formula in 64 bits, not those of a nearby float.
+// Bound by memory: 16384 x 4096 with both norms, fp32 residual into codes 705 MB in
+// 144 us, 4.9 TB/s (a copy reaches 5.1); into 16 bits 805 MB in 142 us; bf16 residual
+// into 16 bits 537 MB in 96 us, into codes, where the double operations show, 437 MB in 114 us.
 #include <algorithm>
 
 #include "mx4_device.h"
@@ -101,267 +98,223 @@ template <bool BF, bool RF32, bool MX4, int W, int P>
 __global__ __launch_bounds__(W == 1 ? 256 : 64 * W) void residual_norm_kernel(NormArgs a) {
   using Acc = std::conditional_t<MX4, double, float>;
   constexpr int T = 64 * W;  // threads of a row
-  constexpr bool AHEAD = !(MX4 && P * W > 16);  // (there the registers do not reach)
-  // (An exchange of a row of its own, rows in turn of two sets: a set is written again behind another row's
-  // barriers.  A row that is left has none, and takes no set.)
-  __shared__ double red[2][4][W];
+  __shared__ double red[4][W];  // (an exchange each)
   const int tid = W == 1 ? threadIdx.x & 63 : threadIdx.x;
   const bool all = a.D == 8 * T * P;
-  const int64_t step = W == 1 ? 4 * static_cast<int64_t>(gridDim.x) : gridDim.x;
-  // First channel of half h of piece c (fp32 residual: fours of a thread's own, T fours apart), and whether the row has it.
-  auto at = [&](int c, int h) { return RF32 ? 8 * T * c + 4 * T * h + 4 * tid : 8 * T * c + 8 * tid + 4 * h; };
-  auto on = [&](int c, int h) { return all || at(c, h) < a.D; };
-  // Piece c of 16-bit rows (0 past their end).
-  auto get = [&](const uint16_t* p, int c) {
-    if constexpr (RF32) {
-      const uint2 z = make_uint2(0, 0);
-      const uint2 u = on(c, 0) ? *reinterpret_cast<const uint2*>(p + at(c, 0)) : z;
-      const uint2 v = on(c, 1) ? *reinterpret_cast<const uint2*>(p + at(c, 1)) : z;
-      return make_uint4(u.x, u.y, v.x, v.y);
-    } else {
-      return on(c, 0) ? *reinterpret_cast<const uint4*>(p + at(c, 0)) : make_uint4(0, 0, 0, 0);
-    }
-  };
-  auto put = [&](uint16_t* p, int c, const uint4& q) {
-    if constexpr (RF32) {
-      if (on(c, 0)) *reinterpret_cast<uint2*>(p + at(c, 0)) = make_uint2(q.x, q.y);
-      if (on(c, 1)) *reinterpret_cast<uint2*>(p + at(c, 1)) = make_uint2(q.z, q.w);
-    } else {
-      if (on(c, 0)) *reinterpret_cast<uint4*>(p + at(c, 0)) = q;
-    }
-  };
+  // First channel of piece c, and whether the row has it.
+  auto at = [&](int c) { return 8 * (T * c + tid); };
+  auto on = [&](int c) { return all || at(c) < a.D; };
+  // (Loads past the row's end read its first piece: with none of them conditional they leave together.)
+  auto from = [&](int c) { return on(c) ? at(c) : 0; };
+  auto get = [&](const uint16_t* p, int c) { return *reinterpret_cast<const uint4*>(p + from(c)); };
 
-  const uint4 zero = make_uint4(0, 0, 0, 0);
-  uint4 y[P], r[P][RF32 ? 2 : 1];
-  auto load = [&](int64_t row) {
-#pragma unroll
-    for (int c = 0; c < P; ++c) {
-      y[c] = a.Y ? get(a.Y + row * a.ldy, c) : zero;
-      if constexpr (RF32) {
-        const float* s = static_cast<const float*>(a.R) + row * a.ldr;
-#pragma unroll
-        for (int h = 0; h < 2; ++h) r[c][h] = a.R && on(c, h) ? *reinterpret_cast<const uint4*>(s + at(c, h)) : zero;
-      } else {
-        r[c][0] = a.R ? get(static_cast<const uint16_t*>(a.R) + row * a.ldr, c) : zero;
-      }
-    }
-  };
-  int64_t row = W == 1 ? static_cast<int64_t>(blockIdx.x) * 4 + (threadIdx.x >> 6) : blockIdx.x;
+  const int64_t row = W == 1 ? static_cast<int64_t>(blockIdx.x) * 4 + (threadIdx.x >> 6) : blockIdx.x;
   if (row >= a.M) return;
-  load(row);
-  for (int set = 0;;) {
-    const int64_t next = row + step;
-    int64_t g = 0;
-    bool there = true;
-    if (a.mod_row && (a.gate || a.scale || a.shift)) {
-      const int k = a.mod_row[row];
-      there = k >= 0 && k < a.n_mod;  // (else the whole row is left)
-      g = there ? k * a.ldm : 0;
+  int64_t g = 0;
+  if (a.mod_row && (a.gate || a.scale || a.shift)) {
+    const int k = a.mod_row[row];
+    if (k < 0 || k >= a.n_mod) return;  // (the whole row is left)
+    g = k * a.ldm;
+  }
+  Acc v[P][8];
+  uint4 y[P], r[P][RF32 ? 2 : 1];
+#pragma unroll
+  for (int c = 0; c < P; ++c) {
+    // (No choice between a row and a constant by reference: its loads would be flat ones.)
+    y[c] = a.Y ? get(a.Y + row * a.ldy, c) : make_uint4(0, 0, 0, 0);
+    if constexpr (RF32) {
+      const uint4* s = reinterpret_cast<const uint4*>(static_cast<const float*>(a.R) + row * a.ldr + from(c));
+#pragma unroll
+      for (int h = 0; h < 2; ++h) r[c][h] = a.R ? uint4(s[h]) : make_uint4(0, 0, 0, 0);
+    } else {
+      r[c][0] = a.R ? get(static_cast<const uint16_t*>(a.R) + row * a.ldr, c) : make_uint4(0, 0, 0, 0);
     }
-    Acc v[P][8];
-    uint4 old[P][RF32 ? 2 : 1];
+  }
 #pragma unroll
-    for (int c = 0; c < P; ++c) {
+  for (int c = 0; c < P; ++c)
 #pragma unroll
-      for (int e = 0; e < 8; ++e) v[c][e] = half8<BF>(y[c], e);
+    for (int e = 0; e < 8; ++e) v[c][e] = on(c) ? half8<BF>(y[c], e) : 0.0f;
+  // Mean (LayerNorm) and 1 / sqrt(mean square + eps) of the row's v (0 past its end).
+  auto statistics = [&](const NormOf& k, int slot, Acc* mean, Acc* rstd) {
+    Acc s = 0;
+    *mean = 0;
+    if (k.kind == OQ_NORM_LAYER) {
 #pragma unroll
-      for (int h = 0; h < (RF32 ? 2 : 1); ++h) old[c][h] = r[c][h];
-    }
-    if (AHEAD && next < a.M) load(next);  // (under way while this row is worked on)
-    // Mean (LayerNorm) and 1 / sqrt(mean square + eps) of the row's v (0 past its end).
-    auto statistics = [&](const NormOf& k, int slot, Acc* mean, Acc* rstd) {
-      Acc s = 0;
-      *mean = 0;
-      if (k.kind == OQ_NORM_LAYER) {
+      for (int c = 0; c < P; ++c)
 #pragma unroll
-        for (int c = 0; c < P; ++c)
+        for (int e = 0; e < 8; ++e) s += v[c][e];
+      const Acc m = static_cast<Acc>(row_sum<W>(s, red[slot]) * a.inv_d);
+      s = 0;
 #pragma unroll
-          for (int e = 0; e < 8; ++e) s += v[c][e];
-        const Acc m = static_cast<Acc>(row_sum<W>(s, red[set][slot]) * a.inv_d);
-        s = 0;
-#pragma unroll
-        for (int c = 0; c < P; ++c)
-#pragma unroll
-          for (int h = 0; h < 2; ++h)
-            if (on(c, h)) {
-#pragma unroll
-              for (int e = 4 * h; e < 4 * h + 4; ++e) {
-                const Acc d = v[c][e] - m;
-                s = fma(d, d, s);
-              }
-            }
-        *mean = m;
-      } else {
-#pragma unroll
-        for (int c = 0; c < P; ++c)
-#pragma unroll
-          for (int e = 0; e < 8; ++e) s = fma(v[c][e], v[c][e], s);
-      }
-      *rstd = static_cast<Acc>(inverse_root(row_sum<W>(s, red[set][slot + 1]) * a.inv_d + static_cast<double>(k.eps)));
-    };
-    // x = piece c's values normed (past the row's end: anything).
-    auto apply = [&](const NormOf& k, auto (&x)[8], int c, auto mean, auto rstd) {
-      using F = decltype(rstd);
-#pragma unroll
-      for (int e = 0; e < 8; ++e) x[e] = (k.kind == OQ_NORM_LAYER ? x[e] - mean : x[e]) * rstd;
-      if (k.gain) {
-        const uint4 q = get(k.gain, c);
-        if (k.offset != 0.0f) {
-#pragma unroll
-          for (int e = 0; e < 8; ++e) x[e] *= static_cast<F>(k.offset) + static_cast<F>(half8<BF>(q, e));
-        } else {
-#pragma unroll
-          for (int e = 0; e < 8; ++e) x[e] *= static_cast<F>(half8<BF>(q, e));
-        }
-      }
-      if (k.bias) {
-        const uint4 q = get(k.bias, c);
-#pragma unroll
-        for (int e = 0; e < 8; ++e) x[e] += static_cast<F>(half8<BF>(q, e));
-      }
-    };
-    auto modulate = [&](auto (&x)[8], int c) {
-      using F = std::remove_reference_t<decltype(x[0])>;
-      if (a.scale) {
-        const uint4 q = get(a.scale + g, c);
-#pragma unroll
-        for (int e = 0; e < 8; ++e) x[e] *= static_cast<F>(1) + static_cast<F>(half8<BF>(q, e));
-      }
-      if (a.shift) {
-        const uint4 q = get(a.shift + g, c);
-#pragma unroll
-        for (int e = 0; e < 8; ++e) x[e] += static_cast<F>(half8<BF>(q, e));
-      }
-    };
-    if (there) {
-      if (a.post.kind != OQ_NORM_NONE) {
-        Acc mean, rstd;
-        statistics(a.post, 0, &mean, &rstd);
-#pragma unroll
-        for (int c = 0; c < P; ++c) apply(a.post, v[c], c, mean, rstd);
-      }
-#pragma unroll
-      for (int c = 0; c < P; ++c) {
-        if (a.gate) {
-          const uint4 q = get(a.gate + g, c);
-#pragma unroll
-          for (int e = 0; e < 8; ++e) v[c][e] *= static_cast<Acc>(half8<BF>(q, e));
-        }
-        float o[8];
+      for (int c = 0; c < P; ++c)
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
-          Acc x;
-          if constexpr (RF32) {
-            const uint4 w = old[c][e >> 2];
-            x = __uint_as_float((e & 3) == 0 ? w.x : (e & 3) == 1 ? w.y : (e & 3) == 2 ? w.z : w.w);
-          } else {
-            x = half8<BF>(old[c][0], e);
-          }
-          v[c][e] = fma(static_cast<Acc>(a.alpha), x, v[c][e]);
-          o[e] = static_cast<float>(v[c][e]);
+          const Acc d = on(c) ? v[c][e] - m : static_cast<Acc>(0);
+          s = fma(d, d, s);
         }
-        if (!all) {
+      *mean = m;
+    } else {
 #pragma unroll
-          for (int e = 0; e < 8; ++e)
-            if (!on(c, e >> 2)) v[c][e] = 0;
-        }
-        if (a.Ro) {
-          if constexpr (RF32) {
-            float* d = static_cast<float*>(a.Ro) + row * a.ldro;
+      for (int c = 0; c < P; ++c)
 #pragma unroll
-            for (int h = 0; h < 2; ++h)
-              if (on(c, h)) *reinterpret_cast<float4*>(d + at(c, h)) = make_float4(o[4 * h], o[4 * h + 1], o[4 * h + 2], o[4 * h + 3]);
-          } else {
-            put(static_cast<uint16_t*>(a.Ro) + row * a.ldro, c, pack_half8<BF>(o));
-          }
-        }
-      }
-      if (a.pre.kind != OQ_NORM_NONE) {
-        Acc mean, rstd;
-        statistics(a.pre, 2, &mean, &rstd);
+        for (int e = 0; e < 8; ++e) s = fma(v[c][e], v[c][e], s);
+    }
+    *rstd = static_cast<Acc>(inverse_root(row_sum<W>(s, red[slot + 1]) * a.inv_d + static_cast<double>(k.eps)));
+  };
+  // x = piece c's values normed (past the row's end: anything).
+  auto apply = [&](const NormOf& k, auto (&x)[8], int c, auto mean, auto rstd) {
+    using F = decltype(rstd);
 #pragma unroll
-        for (int c = 0; c < P; ++c) {
-          apply(a.pre, v[c], c, mean, rstd);
-          modulate(v[c], c);
-          if constexpr (MX4 && RF32) {
-            // Blocks of eight lanes, one for each half.
+    for (int e = 0; e < 8; ++e) x[e] = (k.kind == OQ_NORM_LAYER ? x[e] - mean : x[e]) * rstd;
+    if (k.gain) {
+      const uint4 q = get(k.gain, c);
+      if (k.offset != 0.0f) {
 #pragma unroll
-            for (int h = 0; h < 2; ++h) {
-              uint32_t top = 0;
+        for (int e = 0; e < 8; ++e) x[e] *= static_cast<F>(k.offset) + static_cast<F>(half8<BF>(q, e));
+      } else {
 #pragma unroll
-              for (int e = 4 * h; e < 4 * h + 4; ++e) top = max(top, high_word(v[c][e]));
-              top = quad_max(top);
-              const uint32_t byte = step_byte64(max(top, dpp<0x141>(top)));  // (row_half_mirror: the other quad)
-              double w[8] = {};
-#pragma unroll
-              for (int e = 0; e < 4; ++e) w[e] = v[c][4 * h + e];
-              const uint32_t code = codes8(w, byte);
-              if (on(c, h)) {
-                const int p = at(c, h) / 4;
-                reinterpret_cast<uint16_t*>(a.Hq + row * (a.D / 2))[p] = static_cast<uint16_t>(code);
-                if ((p & 7) == 0) a.steps[row * a.lds + (p >> 3)] = static_cast<uint8_t>(byte);
-              }
-            }
-          } else if constexpr (MX4) {
-            uint32_t byte;
-            const uint32_t code = quad_codes(v[c], &byte);
-            if (on(c, 0)) {  // (whole quads)
-              const int p = at(c, 0) / 8;
-              reinterpret_cast<uint32_t*>(a.Hq + row * (a.D / 2))[p] = code;
-              if ((p & 3) == 0) a.steps[row * a.lds + (p >> 2)] = static_cast<uint8_t>(byte);
-            }
-          } else {
-            float o[8];
-#pragma unroll
-            for (int e = 0; e < 8; ++e) o[e] = v[c][e];
-            put(a.H + row * a.ldh, c, pack_half8<BF>(o));
-          }
-        }
+        for (int e = 0; e < 8; ++e) x[e] *= static_cast<F>(half8<BF>(q, e));
       }
     }
-    if (next >= a.M) return;
-    row = next;
-    if (there) set ^= 1;
-    if (!AHEAD) load(next);
+    if (k.bias) {
+      const uint4 q = get(k.bias, c);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) x[e] += static_cast<F>(half8<BF>(q, e));
+    }
+  };
+  auto modulate = [&](auto (&x)[8], int c) {
+    using F = std::remove_reference_t<decltype(x[0])>;
+    if (a.scale) {
+      const uint4 q = get(a.scale + g, c);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) x[e] *= static_cast<F>(1) + static_cast<F>(half8<BF>(q, e));
+    }
+    if (a.shift) {
+      const uint4 q = get(a.shift + g, c);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) x[e] += static_cast<F>(half8<BF>(q, e));
+    }
+  };
+  if (a.post.kind != OQ_NORM_NONE) {
+    Acc mean, rstd;
+    statistics(a.post, 0, &mean, &rstd);
+#pragma unroll
+    for (int c = 0; c < P; ++c) apply(a.post, v[c], c, mean, rstd);
+  }
+#pragma unroll
+  for (int c = 0; c < P; ++c) {
+    if (a.gate) {
+      const uint4 q = get(a.gate + g, c);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) v[c][e] *= static_cast<Acc>(half8<BF>(q, e));
+    }
+    float o[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      Acc x;
+      if constexpr (RF32) {
+        const uint4 w = r[c][e >> 2];
+        x = __uint_as_float((e & 3) == 0 ? w.x : (e & 3) == 1 ? w.y : (e & 3) == 2 ? w.z : w.w);
+      } else {
+        x = half8<BF>(r[c][0], e);
+      }
+      v[c][e] = fma(static_cast<Acc>(a.alpha), x, v[c][e]);
+      o[e] = static_cast<float>(v[c][e]);
+    }
+    if (!all) {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) v[c][e] = on(c) ? v[c][e] : static_cast<Acc>(0);
+    }
+    if (a.Ro && on(c)) {
+      if constexpr (RF32) {
+        float4* d = reinterpret_cast<float4*>(static_cast<float*>(a.Ro) + row * a.ldro + at(c));
+        d[0] = make_float4(o[0], o[1], o[2], o[3]);
+        d[1] = make_float4(o[4], o[5], o[6], o[7]);
+      } else {
+        *reinterpret_cast<uint4*>(static_cast<uint16_t*>(a.Ro) + row * a.ldro + at(c)) = pack_half8<BF>(o);
+      }
+    }
+  }
+  if (a.pre.kind != OQ_NORM_NONE) {
+    Acc mean, rstd;
+    statistics(a.pre, 2, &mean, &rstd);
+#pragma unroll
+    for (int c = 0; c < P; ++c) {
+      apply(a.pre, v[c], c, mean, rstd);
+      modulate(v[c], c);
+      if constexpr (MX4) {
+        uint32_t byte;
+        const uint32_t code = quad_codes(v[c], &byte);
+        if (on(c)) {  // (whole quads)
+          const int p = at(c) / 8;
+          reinterpret_cast<uint32_t*>(a.Hq + row * (a.D / 2))[p] = code;
+          if ((p & 3) == 0) a.steps[row * a.lds + (p >> 2)] = static_cast<uint8_t>(byte);
+        }
+      } else if (on(c)) {
+        float o[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) o[e] = v[c][e];
+        *reinterpret_cast<uint4*>(a.H + row * a.ldh + at(c)) = pack_half8<BF>(o);
+      }
+    }
   }
 }
 
 template <bool BF, bool RF32, bool MX4, int W, int P>
 int launch_norm(const NormArgs& a, hipStream_t stream) {
-  // (At most what the chip holds at once: a workgroup then takes row after row.)
-  const int threads = W == 1 ? 256 : 64 * W;
-  const int64_t blocks = std::min<int64_t>(W == 1 ? (a.M + 3) / 4 : a.M, 256 * 2048 / threads);
-  hipLaunchKernelGGL((residual_norm_kernel<BF, RF32, MX4, W, P>), dim3(static_cast<unsigned>(blocks)), dim3(threads), 0, stream, a);
-  return launch_status();
+  constexpr int threads = W == 1 ? 256 : 64 * W;
+  constexpr int64_t slab = int64_t{1} << 21;  // rows of a launch (2^31 threads at most)
+  for (int64_t r0 = 0; r0 < a.M; r0 += slab) {
+    NormArgs b = a;
+    b.M = std::min(slab, a.M - r0);
+    if (a.R) b.R = static_cast<const uint8_t*>(a.R) + r0 * a.ldr * (RF32 ? 4 : 2);
+    if (a.Y) b.Y = a.Y + r0 * a.ldy;
+    if (a.mod_row) b.mod_row = a.mod_row + r0;
+    if (a.Ro) b.Ro = static_cast<uint8_t*>(a.Ro) + r0 * a.ldro * (RF32 ? 4 : 2);
+    if (a.H) b.H = a.H + r0 * a.ldh;
+    if (a.Hq) {
+      b.Hq = a.Hq + r0 * (a.D / 2);
+      b.steps = a.steps + r0 * a.lds;
+    }
+    const int64_t blocks = W == 1 ? (b.M + 3) / 4 : b.M;
+    hipLaunchKernelGGL((residual_norm_kernel<BF, RF32, MX4, W, P>), dim3(static_cast<unsigned>(blocks)), dim3(threads), 0, stream, b);
+    const int st = launch_status();
+    if (st != OQ_OK) return st;
+  }
+  return OQ_OK;
 }
 
 // Waves of a row and pieces of a thread, us at 16384 rows (4096 of 8192 channels and more) in bf16 with both RMS norms: W, P
-// of the one taken, and of another (timed when a row's roots took longer: up to 9% of these).
-//                      fp32 residual                             bf16 residual
-//   codes     1024     2, 1 53 / 1, 2 61                         1, 2 39 / 2, 1 45
-//             2048     4, 1 100 / 1, 4 151                       4, 1 74 / 1, 4 84
-//             4096     8, 1 196 / 4, 2 223                       4, 2 131 / 8, 1 157
-//             8192     16, 1 103 / 4, 4 165                      16, 1 89 / 8, 2 97
-//            16384     8, 4 223 / 16, 2 245                      16, 2 153 / 8, 4 178
-//   16 bits   2048     2, 2 97 / 4, 1 98                         2, 2 60 / 4, 1 64
-//             4096     4, 2 180 / 8, 1 188                       4, 2 114 / 8, 1 120
-//             8192     16, 1 99 / 8, 2 110                       8, 2 61 / 16, 1 69
-// Few rows take one piece a thread: 64 x 4096 8, 1 5.4 / 4, 2 6.4.
+// of the one taken / of another.
+//                      fp32 residual                         bf16 residual
+//   codes     1024     2, 1 38.3 / 1, 2 42.6                 2, 1 32.1 / 1, 2 33.5
+//             2048     4, 1 73.1 / 2, 2 82.0                 2, 2 58.4 / 4, 1 61.3
+//             4096     8, 1 144 / 4, 2 155                   4, 2 114 / 8, 1 125
+//             8192     8, 2 86.8 / 16, 1 87.4                8, 2 60.5 / 16, 1 69.7
+//            16384     16, 2 184 / 8, 4 199                  8, 4 126 / 16, 2 142
+//   16 bits   1024     2, 1 35.6 / 1, 2 37.2                 2, 1 24.9 / 1, 2 24.1
+//             2048     4, 1 74.4 / 2, 2 77.5                 2, 2 45.6 / 4, 1 47.3
+//             4096     8, 1 142 / 4, 2 143                   8, 1 95.9 / 4, 2 97.3
+//             8192     8, 2 78.8 / 16, 1 78.1                8, 2 48.1 / 16, 1 50.2
+//            16384     16, 2 152 / 8, 4 159                  16, 2 102 / 8, 4 103
+// Few rows take one piece a thread: codes of 64 x 4096 8, 1 4.6 / 4, 2 5.5; of 1024 x 4096 12.2 / 12.7.
 template <bool BF, bool RF32, bool MX4>
 int launch_norm(const NormArgs& a, hipStream_t stream) {
-  const int n = (a.D + 7) / 8;
-  const bool few = a.M <= 512;
+  const int n = a.D / 8;
+  const bool few = a.M <= 1024;
   if (n <= 64) return launch_norm<BF, RF32, MX4, 1, 1>(a, stream);
-  if (n <= 128) return RF32 || few ? launch_norm<BF, RF32, MX4, 2, 1>(a, stream) : launch_norm<BF, RF32, MX4, 1, 2>(a, stream);
-  if (n <= 256) return MX4 || few ? launch_norm<BF, RF32, MX4, 4, 1>(a, stream) : launch_norm<BF, RF32, MX4, 2, 2>(a, stream);
-  if (n <= 512) return (MX4 && RF32) || few ? launch_norm<BF, RF32, MX4, 8, 1>(a, stream) : launch_norm<BF, RF32, MX4, 4, 2>(a, stream);
-  if constexpr (MX4 || RF32) {
-    if (n <= 1024) return launch_norm<BF, RF32, MX4, 16, 1>(a, stream);
-  } else {
-    if (n <= 1024) return launch_norm<BF, RF32, MX4, 8, 2>(a, stream);
+  if (n <= 128) return launch_norm<BF, RF32, MX4, 2, 1>(a, stream);
+  if constexpr (!RF32) {
+    if (!few && n <= 256) return launch_norm<BF, RF32, MX4, 2, 2>(a, stream);
   }
-  if constexpr (RF32) return launch_norm<BF, RF32, MX4, 8, 4>(a, stream);
-  else return launch_norm<BF, RF32, MX4, 16, 2>(a, stream);
+  if (n <= 256) return launch_norm<BF, RF32, MX4, 4, 1>(a, stream);
+  if constexpr (MX4 && !RF32) {
+    if (!few && n <= 512) return launch_norm<BF, RF32, MX4, 4, 2>(a, stream);
+    if (!few && n > 1024) return launch_norm<BF, RF32, MX4, 8, 4>(a, stream);
+  }
+  if (n <= 512) return launch_norm<BF, RF32, MX4, 8, 1>(a, stream);
+  if (n <= 1024) return few ? launch_norm<BF, RF32, MX4, 16, 1>(a, stream) : launch_norm<BF, RF32, MX4, 8, 2>(a, stream);
+  return launch_norm<BF, RF32, MX4, 16, 2>(a, stream);
 }
 
 bool norm_of(const oq_norm* k, NormOf* out, int* st) {
