@@ -68,8 +68,8 @@ __global__ __launch_bounds__(kThreads) void mx4_quantize_kernel(QuantArgs a) {
 //
 // The stages run in float.  A sum of 2^LOG inputs is then off by at most LOG 2^-24
 // sum|x|, and twice a rounding more follow, so codes that the two ends of that
-// interval share are the exact ones'; a wave that holds another (1 in 50 for
-// blocks of 32, 1 in 15 for 128) repeats its blocks in double, where the sums of
+// interval share are the exact ones'; a wave that holds another (about 1 in 50
+// for blocks of 32, 1 in 15 for 128) repeats its blocks in double, where the sums of
 // fp16 values are exact.  Double for all of them costs twice the operations
 // (16384 x 4096 in blocks of 128: 57 us, so 43).
 template <int LOG, typename F>

@@ -9,8 +9,8 @@
 // and r' and h written once.  A thread holds P pieces of 8 channels of a row, W
 // waves a row (W = 1: four rows a workgroup, and no barrier).  (A workgroup that
 // takes row after row with the next one's loads under way holds more registers
-// and was 3% to 13% slower; pieces of an fp32 residual two fours apart, so that its
-// accesses are of whole kilobytes, cost 4% to 15%.)
+// and was 2% to 12% slower up to 4096 channels, even beyond; pieces of an fp32 residual
+// two fours apart, so that its accesses are of whole kilobytes, cost 4% to 17%.)
 // Sums of a thread's values are float (double where codes are written), sums
 // over threads double.  LayerNorm sums (x - mean)^2 with the mean known: a
 // second exchange, but no cancellation.
