@@ -17,8 +17,8 @@
 // Where codes are written, everything is double: the codes are then those of the
 // formula in 64 bits, not those of a nearby float.
 // Bound by memory: 16384 x 4096 with both norms, fp32 residual into codes 705 MB in
-// 144 us, 4.9 TB/s (a copy reaches 5.1); into 16 bits 805 MB in 142 us; bf16 residual
-// into 16 bits 537 MB in 96 us, into codes, where the double operations show, 437 MB in 114 us.
+// 144-152 us, 4.6-4.9 TB/s (a copy reaches 5.1); into 16 bits 805 MB in 140 us; bf16 residual
+// into 16 bits 537 MB in 96-101 us, into codes, where the double operations show, 437 MB in 114-119 us.
 #include <algorithm>
 
 #include "mx4_device.h"
@@ -130,6 +130,13 @@ __global__ __launch_bounds__(W == 1 ? 256 : 64 * W) void residual_norm_kernel(No
       r[c][0] = a.R ? get(static_cast<const uint16_t*>(a.R) + row * a.ldr, c) : make_uint4(0, 0, 0, 0);
     }
   }
+  // (One piece a thread into 16 bits: the parameters come with the row, 1024 x 1536 with a modulation 9.5 us, so 8.9,
+  // 16384 x 4096 143.6, so 139.4.  Beside doubles they hold too many registers: 151, so 159.)
+  constexpr bool EARLY = P == 1 && !MX4;
+  auto early = [&](const uint16_t* p) { return EARLY && p ? get(p, 0) : make_uint4(0, 0, 0, 0); };
+  const uint4 post_gain = early(a.post.gain), post_bias = early(a.post.bias), gate = early(a.gate ? a.gate + g : nullptr);
+  const uint4 pre_gain = early(a.pre.gain), pre_bias = early(a.pre.bias);
+  const uint4 scale = early(a.scale ? a.scale + g : nullptr), shift = early(a.shift ? a.shift + g : nullptr);
 #pragma unroll
   for (int c = 0; c < P; ++c)
 #pragma unroll
@@ -162,12 +169,12 @@ __global__ __launch_bounds__(W == 1 ? 256 : 64 * W) void residual_norm_kernel(No
     *rstd = static_cast<Acc>(inverse_root(row_sum<W>(s, red[slot + 1]) * a.inv_d + static_cast<double>(k.eps)));
   };
   // x = piece c's values normed (past the row's end: anything).
-  auto apply = [&](const NormOf& k, auto (&x)[8], int c, auto mean, auto rstd) {
+  auto apply = [&](const NormOf& k, const uint4& gain, const uint4& bias, auto (&x)[8], int c, auto mean, auto rstd) {
     using F = decltype(rstd);
 #pragma unroll
     for (int e = 0; e < 8; ++e) x[e] = (k.kind == OQ_NORM_LAYER ? x[e] - mean : x[e]) * rstd;
     if (k.gain) {
-      const uint4 q = get(k.gain, c);
+      const uint4 q = EARLY ? uint4(gain) : get(k.gain, c);
       if (k.offset != 0.0f) {
 #pragma unroll
         for (int e = 0; e < 8; ++e) x[e] *= static_cast<F>(k.offset) + static_cast<F>(half8<BF>(q, e));
@@ -177,7 +184,7 @@ __global__ __launch_bounds__(W == 1 ? 256 : 64 * W) void residual_norm_kernel(No
       }
     }
     if (k.bias) {
-      const uint4 q = get(k.bias, c);
+      const uint4 q = EARLY ? uint4(bias) : get(k.bias, c);
 #pragma unroll
       for (int e = 0; e < 8; ++e) x[e] += static_cast<F>(half8<BF>(q, e));
     }
@@ -185,12 +192,12 @@ __global__ __launch_bounds__(W == 1 ? 256 : 64 * W) void residual_norm_kernel(No
   auto modulate = [&](auto (&x)[8], int c) {
     using F = std::remove_reference_t<decltype(x[0])>;
     if (a.scale) {
-      const uint4 q = get(a.scale + g, c);
+      const uint4 q = EARLY ? uint4(scale) : get(a.scale + g, c);
 #pragma unroll
       for (int e = 0; e < 8; ++e) x[e] *= static_cast<F>(1) + static_cast<F>(half8<BF>(q, e));
     }
     if (a.shift) {
-      const uint4 q = get(a.shift + g, c);
+      const uint4 q = EARLY ? uint4(shift) : get(a.shift + g, c);
 #pragma unroll
       for (int e = 0; e < 8; ++e) x[e] += static_cast<F>(half8<BF>(q, e));
     }
@@ -199,12 +206,12 @@ __global__ __launch_bounds__(W == 1 ? 256 : 64 * W) void residual_norm_kernel(No
     Acc mean, rstd;
     statistics(a.post, 0, &mean, &rstd);
 #pragma unroll
-    for (int c = 0; c < P; ++c) apply(a.post, v[c], c, mean, rstd);
+    for (int c = 0; c < P; ++c) apply(a.post, post_gain, post_bias, v[c], c, mean, rstd);
   }
 #pragma unroll
   for (int c = 0; c < P; ++c) {
     if (a.gate) {
-      const uint4 q = get(a.gate + g, c);
+      const uint4 q = EARLY ? uint4(gate) : get(a.gate + g, c);
 #pragma unroll
       for (int e = 0; e < 8; ++e) v[c][e] *= static_cast<Acc>(half8<BF>(q, e));
     }
@@ -240,7 +247,7 @@ __global__ __launch_bounds__(W == 1 ? 256 : 64 * W) void residual_norm_kernel(No
     statistics(a.pre, 2, &mean, &rstd);
 #pragma unroll
     for (int c = 0; c < P; ++c) {
-      apply(a.pre, v[c], c, mean, rstd);
+      apply(a.pre, pre_gain, pre_bias, v[c], c, mean, rstd);
       modulate(v[c], c);
       if constexpr (MX4) {
         uint32_t byte;
