@@ -477,7 +477,9 @@ int oq_mx4_linear(const uint8_t* Xq, const uint8_t* x_steps, int64_t M, const ui
 /*
  * oq_gated_activation -- h = act(g) u of rows [g | u] as a gate|up linear writes
  * them, act(g) = g / (1 + e^-t), t = g (SiLU) or 2 sqrt(2 / pi) (g + 0.044715 g^3)
- * (GELU in its tanh form), in 16 bits or as the codes of the next linear.
+ * (GELU in its tanh form), in 16 bits or as the codes of the next linear.  (16 bits:
+ * where e^-t is past 2^270, and no finite u makes half the smallest number of act(g) u, act(g)
+ * counts as 0.)
  * GU       device fp16 or bf16 (dtype) [M][ld], g in columns 0 .. F - 1, u in F ..
  *          2 F - 1; ld >= 2 F, % 8 == 0, 16-byte aligned
  * F        % 8 == 0 (codes: % 32), 8 <= F <= OQ_MX4_MAX_K

@@ -235,14 +235,27 @@ __global__ __launch_bounds__(kThreads) void gated_activation_kernel(ActArgs a) {
   const uint32_t r = divide(i, a.row), p = i - r * a.row.d;
   const uint16_t* src = a.GU + r * a.ld + p * 8;
   const uint4 qg = *reinterpret_cast<const uint4*>(src), qu = *reinterpret_cast<const uint4*>(src + a.F);
-  float v[8], rel[8];
+  float v[8], rel[8], x[8], most = 0.0f;
 #pragma unroll
   for (int e = 0; e < 8; ++e) {
     const float g = half8<BF>(qg, e), u = half8<BF>(qu, e), t = act_exponent<ACT>(g);
-    v[e] = g * __builtin_amdgcn_rcpf(1.0f + __expf(-t)) * u;
+    x[e] = t * -1.4426950408889634f;  // e^-t = 2^x
+    most = fmaxf(most, x[e]);
+    v[e] = u * __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(x[e])) * g;
     // Twice what the roundings of t (three of them, and of its product with
     // log2 e) and of the other steps can add up to, relative.
     rel[e] = 2.0f * (fabsf(t) * 0x1p-21f + 0x1p-20f);
+  }
+  // Past x = 126 the reciprocal leaves the normal floats, and u of bf16 can bring the
+  // product back: there 1 + 2^x is 2^x, taken 2^-144 times, and the rest of the power
+  // goes to u and to the result (from x = 270 on 0: act(g) u is below 2^-134 then, half the
+  // smallest bf16).  A wave without such a gate, as nearly all are, does not compute it.
+  if (__any(most > 120.0f)) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      const float far = half8<BF>(qu, e) * 0x1p-72f * __builtin_amdgcn_rcpf(__builtin_amdgcn_exp2f(x[e] - 144.0f)) * half8<BF>(qg, e) * 0x1p-72f;
+      v[e] = x[e] > 120.0f ? far : v[e];
+    }
   }
   if constexpr (!MX4) {
     *reinterpret_cast<uint4*>(static_cast<uint16_t*>(a.H) + r * a.ldh + p * 8) = pack_half8<BF>(v);
