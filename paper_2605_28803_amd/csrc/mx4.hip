@@ -410,8 +410,9 @@ extern "C" int oq_gated_activation(const void* GU, int64_t M, int64_t F, int64_t
   if (H && mx4) return OQ_ERR_ARG;
   int st = OQ_OK;
   if (mx4 && (st = mx4_codes_validate(M, F, Hq, steps)) != OQ_OK) return st;
-  if (!mx4 && ldh < F) return OQ_ERR_SHAPE;
-  if (ld % 8 != 0 || (!mx4 && ldh % 8 != 0)) return OQ_ERR_ALIGN;
+  // (Without rows the codes' pointers may be null too: only an H has a stride.)
+  if (H && ldh < F) return OQ_ERR_SHAPE;
+  if (ld % 8 != 0 || (H && ldh % 8 != 0)) return OQ_ERR_ALIGN;
   if (M == 0) return OQ_OK;
   if (!GU || (!mx4 && !H)) return OQ_ERR_NULL;
   if (!aligned(GU, 16) || (!mx4 && !aligned(H, 16))) return OQ_ERR_ALIGN;
