@@ -187,7 +187,8 @@ def residual_norm(R, Y=None, pre=None, post=None, alpha=1.0, gate=None, scale=No
     or [D], or None; mod_row int32 [M]: their row for each token (None: row 0;
     out of range: the token is skipped).  h is in Y's type (`dtype` where there is
     no Y), or with mx4 the pair (codes, steps) of the next linear.  R_out may be R,
-    H may be Y."""
+    H may be Y.  R_out False: r' is not written (None), as for a first norm whose
+    residual is R itself."""
     first = R if Y is None else Y
     _want(first is not None and first.dim() == 2, "R or Y [M, D] expected")
     M, D = first.shape
@@ -204,7 +205,7 @@ def residual_norm(R, Y=None, pre=None, post=None, alpha=1.0, gate=None, scale=No
         _want(rt is half or rt is torch.float32, "R: Y's type or float32 expected")
         ldr, r = _ld(R, "R", M, D, rt, dev), R.data_ptr()
     else:
-        rt = half if R_out is None else R_out.dtype
+        rt = half if R_out is None or R_out is False else R_out.dtype
         _want(rt is half or rt is torch.float32, "R_out: Y's type or float32 expected")
     of = (half, D, dev)
     _want((pre is None or pre.of in (None, of)) and (post is None or post.of in (None, of)),
@@ -225,10 +226,16 @@ def residual_norm(R, Y=None, pre=None, post=None, alpha=1.0, gate=None, scale=No
         _want(mod_row.dtype is torch.int32 and mod_row.shape == (M,) and mod_row.is_contiguous() and mod_row.get_device() == dev,
               f"mod_row: contiguous int32 [{M}] on cuda:{dev} expected")
         row = mod_row.data_ptr()
-    if R_out is None:
-        R_out, ldro = _empty(first, (M, D), rt, stream), D
+    ldro, ro = D, None
+    if R_out is False:
+        _want(pre is not None, "without pre and R_out there is no output")
+        R_out = None
     else:
-        ldro = _ld(R_out, "R_out", M, D, rt, dev)
+        if R_out is None:
+            R_out = _empty(first, (M, D), rt, stream)
+        else:
+            ldro = _ld(R_out, "R_out", M, D, rt, dev)
+        ro = R_out.data_ptr()
     if pre is None:
         _want(H is None and not mx4, "without pre there is no h")
     elif mx4:
@@ -241,6 +248,6 @@ def residual_norm(R, Y=None, pre=None, post=None, alpha=1.0, gate=None, scale=No
             ldh = _ld(H, "H", M, D, half, dev)
         h = H.data_ptr()
     _check(_lib.load().oq_residual_norm(r, ldr, _DTYPE[rt], y, ldy, dt, M, D, None if post is None else post.ref,
-                                        None if pre is None else pre.ref, alpha, pg, ps, pt, ldm, n_mod, row, R_out.data_ptr(), ldro,
+                                        None if pre is None else pre.ref, alpha, pg, ps, pt, ldm, n_mod, row, ro, ldro,
                                         h, ldh, q, steps, _on(stream, dev)), "oq_residual_norm")
     return R_out, H
