@@ -176,7 +176,8 @@ __global__ __launch_bounds__(64 * WM * WN, EU) void mx4_ring_kernel(Mx4Args a) {
   // NB buffers, then SB times 64 bytes of steps a row (after the K loop: the output
   // tile).  With four buffers under way the next sixteen stages' steps come with them.
   constexpr int SB = NB > 2 ? 2 : 1;
-  __shared__ __attribute__((aligned(16))) uint8_t smem[std::max(NB * BUF + SB * STEPS, OUT == OQ_OUT_F32 ? 0 : BM * TP * 2)];
+  __shared__ __attribute__((aligned(128))) uint8_t smem[std::max(NB * BUF + SB * STEPS, OUT == OQ_OUT_F32 ? 0 : BM * TP * 2)];
+  static_assert(__alignof__(smem) % 128 == 0, "a buffer's second stage is found by flipping bit 6 of an address");
 
   const int tid = threadIdx.x, lane = tid & 63;
   const int wv = __builtin_amdgcn_readfirstlane(tid >> 6);
