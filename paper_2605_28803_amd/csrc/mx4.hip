@@ -9,7 +9,7 @@ namespace {
 
 constexpr int kThreads = 256;
 
-// n / d for n < 2^31 by a multiplication: q = (n * m) >> 32 >> s.
+// n / d for n < 2^31 by a multiplication: q = (n * m) >> (31 + s).
 struct Divisor {
   uint32_t d, m, s;
 };
@@ -242,8 +242,8 @@ __global__ __launch_bounds__(kThreads) void gated_activation_kernel(ActArgs a) {
     x[e] = t * -1.4426950408889634f;  // e^-t = 2^x
     most = fmaxf(most, x[e]);
     v[e] = u * __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(x[e])) * g;
-    // Twice what the roundings of t (three of them, and of its product with
-    // log2 e) and of the other steps can add up to, relative.
+    // Over what the roundings of t, of its product with log2 e and of their constants
+    // (nine at most, 2^-24 each) and of the other steps (seven) can add up to, relative.
     rel[e] = 2.0f * (fabsf(t) * 0x1p-21f + 0x1p-20f);
   }
   // Past x = 126 the reciprocal leaves the normal floats, and u of bf16 can bring the

@@ -44,9 +44,9 @@ __device__ __forceinline__ v8i fragment(const Q& q) {
 // 512 codes in turn, and their sums meet in LDS.  In a unit, lane l holds row l % 16
 // and blocks l / 16, l / 16 + 4, .. + 12: a load takes 64 bytes of each row (with
 // blocks 4 (l / 16) .. + 3, one word of steps as it lies, every lane's 16 bytes were a
-// request of their own: 16 x 16384 x 16384 55 us, so 45).  Two or four row blocks a
-// workgroup, or two units at once, were slower for up to 16 rows and behind the ring
-// for more.
+// request of their own: 16 x 8192 x 8192 18.9 us, so 13.5; 1 x 8192 x 8192 10.9, so
+// 10.1).  Two or four row blocks a workgroup, or two units at once, were slower for up
+// to 16 rows and behind the ring for more.
 template <int OUT, int WAVES>
 __global__ __launch_bounds__(64 * WAVES) void mx4_small_kernel(Mx4Args a) {
   __shared__ float red[WAVES][256];

@@ -17,7 +17,7 @@
 // Where codes are written, everything is double: the codes are then those of the
 // formula in 64 bits, not those of a nearby float.
 // Bound by memory: 16384 x 4096 with both norms, fp32 residual into codes 705 MB in
-// 144-152 us, 4.6-4.9 TB/s (a copy reaches 5.1); into 16 bits 805 MB in 140 us; bf16 residual
+// 144-163 us, 4.3-4.9 TB/s (a copy reaches 5.1); into 16 bits 805 MB in 140 us; bf16 residual
 // into 16 bits 537 MB in 96-101 us, into codes, where the double operations show, 437 MB in 114-119 us.
 #include <algorithm>
 
